@@ -11,6 +11,8 @@
  *   aiq_fold_bn          fold batch-norm into the preceding convolution
  *   aiq_quantize_layer   quantize + pack one layer's weights at 4 / 8 / 16 / 32 bits
  *   aiq_qlinear          y = x * dequant(W)^T for a packed weight matrix (small batch)
+ *   aiq_mx_quantize, aiq_mx_dequantize, aiq_mx_linear, aiq_mx_matmul
+ *                        microscaled 4-bit floating point: a scale for every 32 values instead of one per channel
  *   aiq_model_create     fold, then build the L x {4,8,16,32} bank of packed weights
  *   aiq_forward          logits of one scheme on one image batch
  *   aiq_eval_schemes     top-1 agreement of many schemes on an image set
@@ -154,6 +156,46 @@ size_t aiq_qlinear_workspace_bytes(int N, int K, int bits, int M);
 aiq_status_t aiq_qlinear(const void* packed, const float* scales, const float* bias, int N,
                          int K, int bits, const float* x, int M, float* y, void* workspace,
                          size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point: the storage a large layer takes when one scale per output channel is too coarse
+ * for 4 bits (the paper stores a layer at 4 bits with a uniform quantizer, Section 2.1; here every 32 values have a
+ * scale of their own, 4.25 bits a value).  A row of K values is cut into blocks of 32, the last one filled up with zeros.
+ * A block is 32 codes and one byte s:
+ *     value = element(code) * 2^(s - 127);    s = 255: every value of the block is NaN
+ *     element: bit 3 of the code is the sign, bits 2-0 select 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * Codes: rows of aiq_mx_row_bytes(K) = ceil(K / 128) * 64 bytes, value 2j of a row in the low and 2j + 1 in the high
+ * nibble of its byte j; 32-byte aligned.  Scales: rows of aiq_mx_scale_row_bytes(K) = ceil(K / 512) * 16 bytes, one per
+ * block; 16-byte aligned.  All bytes and nibbles behind the last value or block are zero; the products rely on it.
+ *
+ * dtype: type of the values, AIQ_DTYPE_F32, _F16 (IEEE half) or _BF16.  x_stride, y_stride: elements from one row to the
+ * next (ignored for a single row).  Rows of x may start anywhere, overlap or repeat; rows of y may not overlap.  Sizes are
+ * at least 1.  All calls are asynchronous on `stream` and may be captured into a graph.
+ */
+enum { AIQ_DTYPE_F32 = 0, AIQ_DTYPE_F16 = 1, AIQ_DTYPE_BF16 = 2 };
+size_t aiq_mx_row_bytes(int K);         /* 0 for K <= 0 */
+size_t aiq_mx_scale_row_bytes(int K);   /* 0 for K <= 0 */
+
+/* x -> codes and scales.  s = max(E - 2, 0) with E the exponent field that the block's largest |x| has as a float32, so that
+ * this value lies in [4, 8) * 2^(s - 127) (in less only where s = 0); codes are x * 2^(127 - s) rounded to the nearest
+ * element, halfway cases to the one whose last bit is zero, above 6 to 6.  A block with a NaN or an infinity gets s = 255
+ * and zero codes.  Deterministic; the padding is written too. */
+aiq_status_t aiq_mx_quantize(const void* x, int dtype, int rows, int K, int64_t x_stride, void* codes_out,
+                             void* scales_out, void* stream);
+/* codes and scales -> y: the values above, rounded to nearest even in `dtype` (exact in float32, and in bfloat16). */
+aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales, int rows, int K, int dtype, void* y,
+                               int64_t y_stride, void* stream);
+
+/* The linear layer with microscaled weights:  y[m][n] = sum_k x[m][k] W[n][k] + bias[n],  W [N][K] as codes and scales,
+ * x [M][K] and y [M][N] of `dtype`, bias float32 [N] or NULL.  Sums are float32. */
+size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype);
+aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
+                           int M, int64_t x_stride, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,
+                           void* stream);
+/* The product of two microscaled matrices:  y[m][n] = sum_k A[m][k] B[n][k] + bias[n],  A [M][K] (the activations, by
+ * aiq_mx_quantize), B [N][K] (the weights), y [M][N] of `dtype`.  Products are exact, sums are float32. */
+aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales, int M, const void* b_codes, const void* b_scales, int N,
+                           const float* bias, int K, void* y, int dtype, int64_t y_stride, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * Model description.  Layers are listed in scheme order: entry i of a scheme is the

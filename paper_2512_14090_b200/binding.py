@@ -26,6 +26,8 @@ EXPORTS = [
     "aiq_model_layer_folded", "aiq_model_layer_packed", "aiq_workspace_bytes", "aiq_forward",
     "aiq_eval_schemes", "aiq_set_eval_options", "aiq_set_fusion", "aiq_set_small_pass_images", "aiq_quantize_layer_per_tensor", "aiq_set_scale_granularity", "aiq_last_call_stats", "aiq_scheme_ai",
     "aiq_profile_start", "aiq_profile_stop", "aiq_forward_static",
+    "aiq_mx_row_bytes", "aiq_mx_scale_row_bytes", "aiq_mx_quantize", "aiq_mx_dequantize", "aiq_mx_linear_workspace_bytes",
+    "aiq_mx_linear", "aiq_mx_matmul",
     "aiq_set_compute_path", "aiq_model_status", "aiq_debug_expire_wait", "aiq_search_greedy", "aiq_search_coordinate_descent",
 ]
 
@@ -86,6 +88,21 @@ def _load():
     lib.aiq_qlinear.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, sz, vp]
     lib.aiq_qlinear_workspace_bytes.restype = sz
     lib.aiq_qlinear_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    i64 = C.c_int64
+    lib.aiq_mx_row_bytes.restype = sz
+    lib.aiq_mx_row_bytes.argtypes = [i32]
+    lib.aiq_mx_scale_row_bytes.restype = sz
+    lib.aiq_mx_scale_row_bytes.argtypes = [i32]
+    lib.aiq_mx_quantize.restype = i32
+    lib.aiq_mx_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
+    lib.aiq_mx_dequantize.restype = i32
+    lib.aiq_mx_dequantize.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp]
+    lib.aiq_mx_linear_workspace_bytes.restype = sz
+    lib.aiq_mx_linear_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.aiq_mx_linear.restype = i32
+    lib.aiq_mx_linear.argtypes = [vp, vp, vp, i32, i32, vp, i32, i32, i64, vp, i64, vp, sz, vp]
+    lib.aiq_mx_matmul.restype = i32
+    lib.aiq_mx_matmul.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, i32, i64, vp]
     lib.aiq_model_bytes.restype = sz
     lib.aiq_model_bytes.argtypes = [C.POINTER(ArchDesc)]
     lib.aiq_model_create.restype = i32
@@ -228,6 +245,121 @@ def aiq_qlinear_workspace_bytes(N, K, bits, M):
 def aiq_qlinear(packed, scales, bias, N, K, bits, x, y, workspace=None, stream=None):
     status = lib.aiq_qlinear(_dev(packed), _dev(scales), _dev(bias), int(N), int(K), int(bits), _dev(x), x.shape[0], _dev(y),
                              _dev(workspace), workspace.numel() if workspace is not None else 0, _stream(stream))
+    if status:
+        _check(status)
+
+
+# ------------------------------------------------------------------- microscaled 4 bits
+DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
+_dtypes = None
+
+
+def _dtype(dtype):
+    """AIQ_DTYPE_* of a torch type (or of itself)."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16,
+                   DTYPE_F32: DTYPE_F32, DTYPE_F16: DTYPE_F16, DTYPE_BF16: DTYPE_BF16}
+    code = _dtypes.get(dtype)
+    if code is None:
+        raise ValueError(f"expected float32, float16 or bfloat16, not {dtype}")
+    return code
+
+
+def _mx_rows(t):
+    """(pointer, type, rows, K, row stride) of a CUDA matrix whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError("expected a CUDA matrix")
+    rows, k = t.shape
+    stride, step = t.stride()
+    if step != 1 and k != 1:
+        raise ValueError("expected contiguous rows")
+    return t.data_ptr(), _dtype(t.dtype), rows, k, stride
+
+
+def _mx_held(codes, scales, k):
+    """(codes pointer, scales pointer, rows) of microscaled rows of k values."""
+    c, s = _dev(codes), _dev(scales)
+    rows = codes.shape[0]
+    if tuple(codes.shape) != (rows, (k + 127) // 128 * 64) or tuple(scales.shape) != (rows, (k + 511) // 512 * 16) \
+            or codes.element_size() != 1 or scales.element_size() != 1:
+        raise ValueError(f"expected codes [{rows}][{(k + 127) // 128 * 64}] and scales [{rows}][{(k + 511) // 512 * 16}] in bytes "
+                         f"for rows of {k} values, not {tuple(codes.shape)} and {tuple(scales.shape)}")
+    return c, s, rows
+
+
+def _mx_bias(bias, n):
+    if bias is not None and (bias.numel() != n or bias.element_size() != 4 or not bias.is_floating_point()):
+        raise ValueError(f"expected a float32 bias of {n} values")
+    return _dev(bias)
+
+
+def _mx_device(*tensors):
+    """The launch goes to the current device's stream: every tensor has to lie there."""
+    import torch
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"expected every tensor on the current device, cuda:{device}, not {t.device}")
+
+
+def aiq_mx_row_bytes(K):
+    return int(lib.aiq_mx_row_bytes(int(K)))
+
+
+def aiq_mx_scale_row_bytes(K):
+    return int(lib.aiq_mx_scale_row_bytes(int(K)))
+
+
+def aiq_mx_quantize(x, codes_out, scales_out, stream=None):
+    """x [rows][K] float32, float16 or bfloat16 (rows may have any stride) -> codes_out uint8 [rows][aiq_mx_row_bytes(K)],
+    scales_out uint8 [rows][aiq_mx_scale_row_bytes(K)]."""
+    ptr, dtype, rows, k, stride = _mx_rows(x)
+    c, s, held = _mx_held(codes_out, scales_out, k)
+    if held != rows:
+        raise ValueError(f"{rows} rows into codes of {held}")
+    _mx_device(x, codes_out, scales_out)
+    _check(lib.aiq_mx_quantize(ptr, dtype, rows, k, stride, c, s, _stream(stream)))
+
+
+def aiq_mx_dequantize(codes, scales, y, stream=None):
+    """codes, scales -> y [rows][K] float32, float16 or bfloat16."""
+    ptr, dtype, rows, k, stride = _mx_rows(y)
+    c, s, held = _mx_held(codes, scales, k)
+    if held != rows:
+        raise ValueError(f"codes of {held} rows into {rows}")
+    _mx_device(y, codes, scales)
+    _check(lib.aiq_mx_dequantize(c, s, rows, k, dtype, ptr, stride, _stream(stream)))
+
+
+def aiq_mx_linear_workspace_bytes(N, K, M, dtype):
+    return int(lib.aiq_mx_linear_workspace_bytes(int(N), int(K), int(M), _dtype(dtype)))
+
+
+def aiq_mx_linear(codes, scales, bias, x, y, workspace=None, stream=None):
+    """y [M][N] = x [M][K] * W^T + bias; W [N][K] as codes and scales, x and y of one type, bias float32 [N] or None."""
+    xp, dtype, m, k, x_stride = _mx_rows(x)
+    yp, y_dtype, y_rows, n, y_stride = _mx_rows(y)
+    c, s, held = _mx_held(codes, scales, k)
+    if (y_dtype, y_rows, held) != (dtype, m, n):
+        raise ValueError(f"x {tuple(x.shape)} {x.dtype}, weights of {held} rows and y {tuple(y.shape)} {y.dtype} do not match")
+    _mx_device(x, y, codes, scales, bias, workspace)
+    status = lib.aiq_mx_linear(c, s, _mx_bias(bias, n), n, k, xp, dtype, m, x_stride, yp, y_stride, _dev(workspace),
+                               workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream(stream))
+    if status:
+        _check(status)
+
+
+def aiq_mx_matmul(a_codes, a_scales, b_codes, b_scales, bias, K, y, stream=None):
+    """y [M][N] = A [M][K] * B [N][K]^T + bias; both matrices as codes and scales, y float32, float16 or bfloat16."""
+    yp, dtype, m, n, y_stride = _mx_rows(y)
+    ac, as_, a_rows = _mx_held(a_codes, a_scales, K)
+    bc, bs, b_rows = _mx_held(b_codes, b_scales, K)
+    if (a_rows, b_rows) != (m, n):
+        raise ValueError(f"A of {a_rows} rows, B of {b_rows} and y {tuple(y.shape)} do not match")
+    _mx_device(y, a_codes, a_scales, b_codes, b_scales, bias)
+    status = lib.aiq_mx_matmul(ac, as_, m, bc, bs, n, _mx_bias(bias, n), int(K), yp, dtype, y_stride, _stream(stream))
     if status:
         _check(status)
 

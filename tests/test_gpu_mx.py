@@ -1,0 +1,188 @@
+"""Microscaled 4-bit operators on the GPU against the float64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import binding
+from mx_util import PIECES, TYPES, activations, check, held, linear, values, weights
+from oracle import mx_oracle as X
+
+pytestmark = pytest.mark.gpu
+
+
+def _special(rows, k, dtype):
+    """Rows that meet every rule of the quantizer: halfway cases, zeros, subnormal numbers, the largest, NaN, infinities."""
+    g = torch.Generator().manual_seed(rows * 1000 + k)
+    x = torch.randn((rows, k), generator=g) * torch.exp(3 * torch.randn((rows, 1), generator=g))
+    ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, -0.25, -0.75, -2.5, -5.0, 7.0, 7.5, 0.0, -0.0])
+    x = x.to(dtype)
+    big = torch.finfo(dtype).max
+    for r in range(rows):
+        if r % 4 == 1:
+            x[r] = ties.repeat(k // 16 + 1)[:k].to(dtype)
+        if r % 4 == 2:
+            x[r, ::3] = 0
+            x[r, : min(k, 40)] = torch.finfo(dtype).smallest_normal / 4
+        if r % 8 == 3:
+            x[r, -1] = big
+        if r % 8 == 7:
+            x[r, k // 2] = [float("nan"), float("inf"), -float("inf")][r % 3]
+    return x
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("rows,k,pad,skip", [(1, 1, 0, 0), (9, 31, 0, 0), (8, 32, 0, 0), (17, 33, 3, 1), (16, 127, 0, 0), (24, 128, 8, 0),
+                                             (24, 129, 7, 5), (9, 511, 1, 1), (16, 512, 0, 0), (11, 513, 0, 0), (40, 1280, 0, 0),
+                                             (7, 1283, 5, 5), (8, 2056, 8, 8)])
+def test_quantize(dtype, rows, k, pad, skip):
+    dt = TYPES[dtype]
+    wide = torch.zeros((rows, k + pad), dtype=dt)
+    wide[:, skip:skip + k] = _special(rows, k, dt)
+    x = wide.cuda()[:, skip:skip + k]
+    codes, scales = held(x)
+    ref_codes, ref_scales = X.quantize(x.cpu().double().numpy())
+    assert np.array_equal(scales.cpu().numpy(), ref_scales)
+    assert np.array_equal(codes.cpu().numpy(), ref_codes)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("rows,k,pad", [(1, 1, 0), (9, 31, 0), (8, 32, 8), (17, 33, 3), (24, 129, 7), (16, 512, 0), (11, 513, 0), (40, 1281, 0),
+                                        (8, 2056, 8)])
+def test_dequantize(dtype, rows, k, pad):
+    b, dt = binding(), TYPES[dtype]
+    codes, scales = held(_special(rows, k, torch.float32).cuda())
+    if rows > 1:
+        scales[0, 0] = 254
+        scales[1, 0] = 0
+    wide = torch.full((rows, k + pad), 7.0, dtype=dt, device="cuda")
+    b.aiq_mx_dequantize(codes, scales, wide[:, :k])
+    with np.errstate(over="ignore"):
+        ref = torch.from_numpy(values(codes, scales, k).astype(np.float32)).to(dt)
+    got = wide.cpu()
+    assert torch.equal(torch.isnan(got[:, :k]), torch.isnan(ref))
+    assert torch.equal(torch.nan_to_num(got[:, :k]), torch.nan_to_num(ref))
+    assert (got[:, k:] == 7.0).all()
+
+
+def test_every_code_and_scale():
+    """All 256 bytes of codes under all 256 scale bytes."""
+    b = binding()
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1).cuda()            # 512 values a row
+    scales = torch.arange(256, dtype=torch.uint8).repeat(16, 1).t().contiguous().cuda()
+    y = torch.empty((256, 512), device="cuda")
+    b.aiq_mx_dequantize(codes, scales, y)
+    with np.errstate(over="ignore"):
+        ref = torch.from_numpy(values(codes, scales, 512).astype(np.float32))
+    assert torch.equal(torch.nan_to_num(y.cpu()), torch.nan_to_num(ref)) and torch.equal(torch.isnan(y.cpu()), torch.isnan(ref))
+
+
+SHAPES = [(1, 1, 1), (3, 33, 2), (8, 32, 1), (10, 64, 1), (129, 100, 5), (64, 320, 9), (200, 609, 17), (128, 512, 33), (1280, 320, 1),
+          (1000, 1281, 4), (257, 2500, 130), (512, 1024, 300), (384, 4097, 64), (130, 8192, 3)]
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n,k,m", SHAPES)
+@pytest.mark.parametrize("workspace", [True, False])
+def test_linear(dtype, n, k, m, workspace):
+    dt = TYPES[dtype]
+    codes, scales = held(weights(n, k, n + k))
+    x = activations(m, k, dt, m + k)
+    bias = torch.randn(n, generator=torch.Generator().manual_seed(3)).cuda() if (n + m) % 2 else None
+    y = linear(codes, scales, bias, x, torch.full((m, n), float("nan"), dtype=dt, device="cuda"), workspace)
+    check(y, x.double().cpu().numpy(), values(codes, scales, k), bias.cpu().numpy() if bias is not None else None, dt, dtype)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n,k,m", SHAPES)
+def test_matmul(dtype, n, k, m):
+    b, dt = binding(), TYPES[dtype]
+    bc, bs = held(weights(n, k, n + k))
+    ac, as_ = held(activations(m, k, torch.float32, m + k))
+    bias = torch.randn(n, generator=torch.Generator().manual_seed(3)).cuda() if (n + m) % 2 else None
+    y = torch.full((m, n), float("nan"), dtype=dt, device="cuda")
+    b.aiq_mx_matmul(ac, as_, bc, bs, bias, k, y)
+    check(y, values(ac, as_, k), values(bc, bs, k), bias.cpu().numpy() if bias is not None else None, dt, "mx")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("m", [1, 3, 20, 150])
+def test_strides_and_what_lies_around(dtype, m):
+    """x a slice of wider rows, or one row repeated; y a slice whose surroundings stay as they were."""
+    dt, n, k = TYPES[dtype], 300, 700
+    codes, scales = held(weights(n, k, 5))
+    w = values(codes, scales, k)
+    for skip, pad in ((0, 0), (1, 4), (8, 8), (3, 13)):
+        x = activations(m, skip + k + pad, dt, 7)[:, skip:skip + k]
+        wide = torch.full((m + 2, n + 9), 7.0, dtype=dt, device="cuda")
+        linear(codes, scales, None, x, wide[1:m + 1, 4:4 + n])
+        check(wide[1:m + 1, 4:4 + n], x.double().cpu().numpy(), w, None, dt, dtype, f"skip {skip}")
+        wide[1:m + 1, 4:4 + n] = 7.0
+        assert (wide == 7.0).all()
+    x = activations(1, k, dt, 8).expand(m, k)
+    y = linear(codes, scales, None, x, torch.empty((m, n), dtype=dt, device="cuda"))
+    check(y, x.double().cpu().numpy(), w, None, dt, dtype, "repeated row")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("m", [1, 40])
+def test_values_of_every_size(dtype, m):
+    """Blocks of x and of W whose sizes lie far apart, all-zero blocks and rows, weights near both ends of the scales."""
+    dt, n, k = TYPES[dtype], 160, 640
+    w = weights(n, k, 11).cpu()
+    w[0] = 0
+    w[1] *= 2.0 ** -110
+    w[2] *= 2.0 ** 100
+    w[3, 32:64] *= 2.0 ** 30
+    w[4, ::2] = 0
+    x = activations(m, k, torch.float32, 12).cpu()
+    x[:, 64:96] *= 2.0 ** -12
+    x[:, 96:128] *= 2.0 ** 8
+    x[:, 128:160] = 0
+    x[0, 200:300] = 0
+    x = x.to(dt).cuda()
+    codes, scales = held(w.cuda())
+    y = linear(codes, scales, None, x, torch.empty((m, n), dtype=dt, device="cuda"))
+    wv = values(codes, scales, k)
+    rows = [i for i in range(n) if dtype != "f16" or i not in (2, 3)]        # these two leave the range of halves
+    check(y[:, rows], x.double().cpu().numpy(), wv[rows], None, dt, dtype)
+    if dtype == "f16":
+        assert torch.isinf(y[:, 2]).all()
+    assert (y[:, 0] == 0).all()
+
+
+@pytest.mark.parametrize("m", [1, 24])
+def test_nan_scales_and_nonfinite_activations_stay_in_their_rows(m):
+    dt, n, k = torch.float32, 140, 300
+    w = weights(n, k, 21)
+    w[5, 40] = float("nan")
+    codes, scales = held(w)
+    x = activations(m, k, dt, 22)
+    if m > 3:
+        x[2, 17] = float("nan")
+        x[3, 299] = float("inf")
+    y = linear(codes, scales, None, x, torch.empty((m, n), dtype=dt, device="cuda"))
+    assert torch.isnan(y[:, 5]).all()
+    keep = [i for i in range(m) if m <= 3 or i not in (2, 3)]
+    cols = [i for i in range(n) if i != 5]
+    if m > 3:
+        assert torch.isnan(y[2]).all() and not torch.isfinite(y[3]).any()
+    check(y[keep][:, cols], x[keep].double().cpu().numpy(), values(codes, scales, k)[cols], None, dt, "f32")
+
+
+def test_quantize_activations_then_multiply():
+    """The operators in a run: weights quantized once, each batch quantized, multiplied, compared with the product of what the
+    codes stand for and with the layer that quantizes its weights alone."""
+    b = binding()
+    n, k, m = 512, 1000, 50
+    w, x = weights(n, k, 31), activations(m, k, torch.bfloat16, 32)
+    wc, ws = held(w)
+    xc, xs = held(x)
+    wv = torch.empty((n, k), device="cuda")
+    xv = torch.empty((m, k), dtype=torch.bfloat16, device="cuda")
+    b.aiq_mx_dequantize(wc, ws, wv)
+    b.aiq_mx_dequantize(xc, xs, xv)
+    y = torch.empty((m, n), device="cuda")
+    b.aiq_mx_matmul(xc, xs, wc, ws, None, k, y)
+    check(y, xv.double().cpu().numpy(), wv.double().cpu().numpy(), None, torch.float32, "mx")
+    z = linear(wc, ws, None, xv.float(), torch.empty((m, n), device="cuda"))
+    check(z, xv.double().cpu().numpy(), wv.double().cpu().numpy(), None, torch.float32, "f32")
