@@ -408,14 +408,13 @@ extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales,
 }
 
 extern "C" size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype) {
-  (void)N; (void)K; (void)M; (void)dtype;
-  return 0;
+  if (N <= 0 || K <= 0 || M <= 0 || !aiq::mx_dtype_ok(dtype)) return 0;
+  return aiq::mx_tc_workspace_bytes(K, M, dtype);
 }
 
 extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
                                       int M, int64_t x_stride, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,
                                       void* stream) {
-  (void)workspace; (void)workspace_bytes;
   if (aiq_status_t st = mx_check("aiq_mx_linear", codes, scales, N, K)) return st;
   if (M <= 0) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear: M=%d", M);
   if (aiq_status_t st = mx_check_rows("aiq_mx_linear", x, dtype, x_stride)) return st;
@@ -429,6 +428,13 @@ extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, con
   p.x = x; p.x_stride = x_stride;
   p.y = y; p.y_stride = y_stride;
   p.N = N; p.K = K; p.M = M; p.dtype = dtype;
+  if (workspace) {
+    if (((uintptr_t)workspace) & 15) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear: workspace not 16-byte aligned");
+    if (workspace_bytes < aiq::mx_tc_workspace_bytes(K, M, dtype))
+      return set_error(AIQ_ERR_WORKSPACE_TOO_SMALL, "aiq_mx_linear: workspace of %zu bytes, %zu needed", workspace_bytes,
+                       aiq::mx_tc_workspace_bytes(K, M, dtype));
+    return aiq::launch_mx_product_tc(p, workspace, (cudaStream_t)stream);
+  }
   return aiq::launch_mx_product_plain(p, (cudaStream_t)stream);
 }
 
@@ -447,5 +453,5 @@ extern "C" aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales,
   p.x_scales = static_cast<const uint8_t*>(a_scales);
   p.y = y; p.y_stride = y_stride;
   p.N = N; p.K = K; p.M = M; p.dtype = dtype;
-  return aiq::launch_mx_product_plain(p, (cudaStream_t)stream);
+  return aiq::launch_mx_product_tc(p, nullptr, (cudaStream_t)stream);
 }

@@ -1,0 +1,615 @@
+// Products of microscaled 4-bit matrices on the tcgen05 tensor cores, which multiply codes and block scales as they are stored.
+//
+//   y[m][n] = sum_k x[m][k] W[n][k] + bias[n]
+//
+// The weights are the MMA's M operand (128 output channels per CTA) and the rows of x its N operand, so that the packed weights
+// - the bytes that bound a small batch - are read once and a single row of x costs one narrow MMA:
+//   D[128 n][R] += (A[128 n][k] 2^sa) (B[R][k] 2^sb)^T
+// KIND 0 (aiq_mx_matmul): both operands are four-bit codes, kind::mxf4, 64 k per MMA, rows of 128 bytes = 256 k.
+// KIND 1 (aiq_mx_linear): x enters as a sum of eight-bit floats (1 + 4 + 3 bits) with a scale per block of 32, kind::mxf8f6f4,
+//   32 k per MMA; TMA expands the weights' codes to a byte each on the way to shared memory.  Each such piece takes the next
+//   five bits of the values (four, and the sign of what is left), so that 2 / 3 / 5 of them hold a bfloat16 / half / float
+//   exactly, unless it lies far below the largest value of its block: 2^-(12 + 5 pieces) of that one is what is lost at most.
+//   The pieces are rows of the B operand beside each other while they fit into 256 (then each has columns of its own
+//   in the sums), or further MMAs into the same columns.
+//   A pre-pass writes them into the workspace; the product starts under programmatic dependent launch and loads weights meanwhile.
+// Products are exact.  The tensor core drops what an addition has below the accumulator's last bit; with float32 results the
+// sums are therefore taken out every 512 k and added up in float32 registers (two sets of columns, used in turn).
+//
+//   warp 0     TMA: weights            warp 2   TMA: rows of x
+//   warp 1     MMA issuer              warp 3   TMA: scale bytes of both, 512 k at a time (16 bytes a row)
+//   warps 4-7  scale bytes: shared memory -> tensor memory, where the MMA reads them: four k blocks of a row in a column's
+//              32-bit word, rows 32 to a column, the same in each quarter of the lanes
+//   warps 8-11 sums: tensor memory -> registers / shared memory
+// A K range may be split over the CTAs of a cluster; their sums meet in shared memory in a fixed order.
+#include "mx.cuh"
+#include "tc_ptx.cuh"
+
+namespace aiq {
+namespace {
+
+constexpr int kMxTcThreads = 12 * 32;
+constexpr int kMxATile = 128 * 128;          // bytes of 128 rows of weights in shared memory
+constexpr int kMxACopied = 128 * 64;         // bytes that a copy counts which expands four-bit codes: those of the codes
+constexpr int kMxSuper = 512;                // k per set of scale bytes
+constexpr int kMxScaleStages = 3;            // sets of scale bytes in shared memory
+constexpr int kMxMaxStages = 12;
+
+template <int KIND>
+struct MxKind {
+  static constexpr int CHUNK = KIND == 0 ? 256 : 128;       // k per 128 bytes of a row in shared memory
+  static constexpr int CPS = kMxSuper / CHUNK;
+};
+
+struct MxTcParams {
+  int N, M;
+  int Mt;                   // rows of x per tile
+  int pieces;               // KIND 1: eight-bit pieces of x
+  int stack;                // 1: the pieces' rows are one operand
+  int rows;                 // rows of a B operand: Mt, stacked pieces * Mt
+  int n_chunks, supers_per_split;
+  int cluster;
+  int a_stages, b_stages;
+  int b_cols;               // scale columns of a B operand (a multiple of 4)
+  int sf_col, sf_group;     // first scale column, columns per 128 k
+  int tmem_cols;
+};
+
+__host__ __device__ inline int mx_b_unit(int rows) { return rows * 128; }
+// rings of codes, then the sums of the tile in their place; [row of x][128 channels]
+__host__ __device__ inline int mx_ring_bytes(const MxTcParams& p) {
+  const int rings = p.a_stages * kMxATile + p.b_stages * mx_b_unit(p.rows), sums = p.Mt * 128 * 4;
+  return rings > sums ? rings : sums;
+}
+__host__ __device__ inline int mx_scale_tile(const MxTcParams& p) { return (128 + p.b_cols * 32 * (p.stack ? 1 : p.pieces)) * 16; }
+inline int mx_smem_bytes(const MxTcParams& p) {
+  return 1024 + mx_ring_bytes(p) + kMxScaleStages * mx_scale_tile(p) + 8 * (2 * p.a_stages + 2 * p.b_stages + 2 * kMxScaleStages + 10) + 16 + 512;
+}
+
+// one MMA; the scale columns and their byte in the words are part of the call
+template <int KIND>
+__device__ __forceinline__ void mx_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  if (KIND == 0)
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void tma_load_2d_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+      "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n\t}"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n\t}"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+// A ring of copies as its producer sees it: wait for the slot, remember the copy; drain() before the CTA may end.
+struct RingCursor {
+  uint32_t stage = 0, phase = 0, issued = 0, issued_phase = 0;
+  __device__ __forceinline__ void sent(uint32_t stages) {
+    issued |= 1u << stage;
+    issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
+    if (++stage == stages) { stage = 0; phase ^= 1u; }
+  }
+  __device__ __forceinline__ void drain(uint32_t full, int stages) const {
+    for (int i = 0; i < stages; ++i)
+      if (issued & (1u << i)) {
+        const long long t0 = clock64();
+        while (!mbar_try_wait(full + 8 * i, (issued_phase >> i) & 1u) && clock64() - t0 < kWaitLimitCycles) {}
+      }
+  }
+};
+
+template <int KIND, typename T>
+__global__ void __launch_bounds__(kMxTcThreads, 1)
+mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ CUtensorMap sa_map,
+             const __grid_constant__ CUtensorMap sb_map, const __grid_constant__ MxTcParams p, const float* __restrict__ bias,
+             T* __restrict__ y, int64_t y_stride, int vec) {
+  using Kd = MxKind<KIND>;
+  constexpr bool PROMOTE = sizeof(T) == 4;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = blockIdx.x % p.cluster;
+  const int n0 = (int)(blockIdx.x / p.cluster) * 128, m0 = blockIdx.y * p.Mt;
+  const int a_stages = p.a_stages, b_stages = p.b_stages, units = p.stack ? 1 : p.pieces;
+  const int b_unit = mx_b_unit(p.rows), scale_tile = mx_scale_tile(p);
+  const int c_begin = min(p.n_chunks, rank * p.supers_per_split * Kd::CPS);
+  const int c_end = min(p.n_chunks, c_begin + p.supers_per_split * Kd::CPS);
+  const int chunks = c_end - c_begin, supers = (chunks + Kd::CPS - 1) / Kd::CPS;
+
+  uint8_t* aring = smem;
+  uint8_t* bring = aring + a_stages * kMxATile;
+  uint8_t* sring = smem + mx_ring_bytes(p);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sring + kMxScaleStages * scale_tile);
+  const uint32_t a_full = smem_u32(bars), a_empty = a_full + 8 * a_stages;
+  const uint32_t b_full = a_empty + 8 * a_stages, b_empty = b_full + 8 * b_stages;
+  const uint32_t s_full = b_empty + 8 * b_stages, s_empty = s_full + 8 * kMxScaleStages;    // scale bytes in shared memory
+  const uint32_t t_full = s_empty + 8 * kMxScaleStages, t_empty = t_full + 16;              // scale words in tensor memory
+  const uint32_t d_full = t_empty + 16, d_empty = d_full + 16;                              // sums
+  const uint32_t retired = d_empty + 16;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 2 * a_stages + 2 * b_stages + 2 * kMxScaleStages + 10);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
+  float* s_bias = reinterpret_cast<float*>(s_tmem + 4);
+
+  if (tid == 0) {
+    for (int i = 0; i < a_stages; ++i) { mbar_init(a_full + 8 * i, 1); mbar_init(a_empty + 8 * i, 1); }
+    for (int i = 0; i < b_stages; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
+    for (int i = 0; i < kMxScaleStages; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_empty + 8 * i, 4); }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(t_full + 8 * i, 4);
+      mbar_init(t_empty + 8 * i, 1);
+      mbar_init(d_full + 8 * i, 1);
+      mbar_init(d_empty + 8 * i, 4);
+    }
+    mbar_init(retired, 1);
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (tid >= 256) {
+    const int n = n0 + tid - 256;
+    s_bias[tid - 256] = bias && n < p.N ? bias[n] : 0.f;
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tmem_alloc(smem_u32(s_tmem), (uint32_t)p.tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *s_tmem;
+  bool alive = true;
+
+  if (warp == 0) {
+    RingCursor r;
+    for (int c = c_begin; c < c_end; ++c) {
+      alive = mbar_wait_warp(a_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+      if (!alive) break;
+      tma_fill_2d(smem_u32(aring) + r.stage * kMxATile, &a_map, a_full + 8 * r.stage, KIND == 0 ? kMxATile : kMxACopied, c * 128, n0);
+      r.sent(a_stages);
+    }
+    r.drain(a_full, a_stages);
+  } else if (warp == 2) {
+    if (KIND == 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+    RingCursor r;
+    for (int c0 = c_begin; c0 < c_end && alive; c0 += Kd::CPS)
+      for (int u = units - 1; u >= 0 && alive; --u)
+        for (int c = c0; c < min(c0 + Kd::CPS, c_end); ++c) {
+          alive = mbar_wait_warp(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+          if (!alive) break;
+          tma_fill_3d(smem_u32(bring) + r.stage * b_unit, &b_map, b_full + 8 * r.stage, (uint32_t)b_unit, c * 128, m0, u);
+          r.sent(b_stages);
+        }
+    r.drain(b_full, b_stages);
+  } else if (warp == 3) {
+    if (KIND == 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+    RingCursor r;
+    for (int s = 0; s < supers; ++s) {
+      alive = mbar_wait_warp(s_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+      if (!alive) break;
+      const uint32_t dst = smem_u32(sring) + r.stage * scale_tile, bar = s_full + 8 * r.stage;
+      const int byte = (c_begin / Kd::CPS + s) * 16;
+      expect_tx_elect(bar, (uint32_t)((128 + p.rows * units) * 16));
+      tma_load_2d_elect(dst, &sa_map, bar, byte, n0);
+      for (int u = 0; u < units; ++u) tma_load_3d_elect(dst + (128 + u * p.b_cols * 32) * 16, &sb_map, bar, byte, m0, u);
+      r.sent(kMxScaleStages);
+    }
+    r.drain(s_full, kMxScaleStages);
+  } else if (warp == 1) {
+    // ---- MMA issuer: all 32 lanes converged, one elected lane issues --------------------------------
+    constexpr uint32_t DESC_HI = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);   // SBO 1024, version 1, 128-byte swizzle
+    constexpr uint32_t LBO_FIELD = 1u << 16;
+    // operand types, N, scales in powers of two, M = 128
+    const uint32_t idesc = (KIND == 0 ? (1u << 7) | (1u << 10) : (5u << 7)) | ((uint32_t)(p.rows >> 3) << 17) | (1u << 23) | (1u << 27);
+    // The smallest pieces come first: while they are added up the sums are small, and so is what the additions drop.
+    uint32_t as = 0, aph = 0, bs = 0, bph = 0;
+    for (int s = 0; s < supers && alive; ++s) {
+      const uint32_t tb = s & 1, tph = (s >> 1) & 1;
+      uint32_t accumulate = !PROMOTE && s > 0;
+      if (PROMOTE) alive = mbar_wait_warp(d_empty + 8 * tb, tph ^ 1u, s_abort, nullptr);
+      alive = alive && mbar_wait_warp(t_full + 8 * tb, tph, s_abort, nullptr);
+      const uint32_t d = tmem_base + (PROMOTE ? tb * p.rows : 0);
+      const uint32_t sf = tmem_base + p.sf_col + tb * 4 * p.sf_group;
+      const int n = min(Kd::CPS, chunks - s * Kd::CPS);
+      for (int u = units - 1; u >= 0 && alive; --u) {
+        uint32_t at = as, atph = aph;
+        for (int cc = 0; cc < n; ++cc) {
+          alive = (u != units - 1 || mbar_wait_warp(a_full + 8 * at, atph, s_abort, nullptr)) &&
+                  mbar_wait_warp(b_full + 8 * bs, bph, s_abort, nullptr);
+          if (!alive) break;
+          tc_fence_after();
+          const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(aring) + at * kMxATile) >> 4) | LBO_FIELD);
+          const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(bring) + bs * b_unit) >> 4) | LBO_FIELD);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t group = KIND == 0 ? 2 * cc + (i >> 1) : cc, id = KIND == 0 ? (i & 1) * 2 : i;
+            const uint32_t sfa = sf + group * p.sf_group;
+            mx_mma<KIND>(d, adesc + 2 * i, bdesc + 2 * i, idesc | (id << 4) | (id << 29), sfa, sfa + 4 + u * p.b_cols, accumulate);
+            accumulate = 1;
+          }
+          umma_commit(b_empty + 8 * bs);
+          if (++bs == (uint32_t)b_stages) { bs = 0; bph ^= 1u; }
+          if (u == 0) umma_commit(a_empty + 8 * at);
+          if (++at == (uint32_t)a_stages) { at = 0; atph ^= 1u; }
+        }
+        if (u == 0) { as = at; aph = atph; }
+      }
+      if (!alive) break;
+      umma_commit(t_empty + 8 * tb);
+      if (PROMOTE || s + 1 == supers) umma_commit(d_full + 8 * (PROMOTE ? tb : 0));
+    }
+    if (!alive) {                                  // what was issued must end before the CTA does
+      umma_commit(retired);
+      const long long t0 = clock64();
+      while (!mbar_try_wait(retired, 0) && clock64() - t0 < kWaitLimitCycles) {}
+    }
+  } else if (warp < 8) {
+    // ---- scale bytes -> tensor memory ----------------------------------------------------------------
+    const uint32_t quarter = (uint32_t)(warp & 3) * 32;
+    const int cols = p.b_cols * units;
+    uint32_t stage = 0, phase = 0;
+    for (int s = 0; s < supers; ++s) {
+      const uint32_t tb = s & 1, tph = (s >> 1) & 1;
+      alive = mbar_wait_warp(s_full + 8 * stage, phase, s_abort, nullptr) && mbar_wait_warp(t_empty + 8 * tb, tph ^ 1u, s_abort, nullptr);
+      if (!alive) break;
+      tc_fence_after();
+      const uint32_t src = smem_u32(sring) + stage * scale_tile + lane * 16;
+      const uint32_t dst = tmem_base + p.sf_col + tb * 4 * p.sf_group + (quarter << 16);
+      for (int c = 0; c < 4 + cols; c += 4) {
+        const uint4 v0 = lds128(src + (c * 32) * 16), v1 = lds128(src + (c * 32 + 32) * 16), v2 = lds128(src + (c * 32 + 64) * 16),
+                    v3 = lds128(src + (c * 32 + 96) * 16);
+        tmem_st4(dst + c, v0.x, v1.x, v2.x, v3.x);
+        tmem_st4(dst + p.sf_group + c, v0.y, v1.y, v2.y, v3.y);
+        tmem_st4(dst + 2 * p.sf_group + c, v0.z, v1.z, v2.z, v3.z);
+        tmem_st4(dst + 3 * p.sf_group + c, v0.w, v1.w, v2.w, v3.w);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(s_empty + 8 * stage);
+        mbar_arrive(t_full + 8 * tb);
+      }
+      if (++stage == kMxScaleStages) { stage = 0; phase ^= 1u; }
+    }
+  } else {
+    // ---- sums -----------------------------------------------------------------------------------------
+    const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+    const int copies = p.stack ? p.pieces : 1;                 // columns that belong to one row of x
+    float* sums = reinterpret_cast<float*>(smem) + (warp & 3) * 32 + lane;
+    if (PROMOTE) {
+      float acc[128];
+#pragma unroll
+      for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+      for (int s = 0; s < supers; ++s) {
+        const uint32_t dbuf = s & 1, dph = (s >> 1) & 1;
+        alive = mbar_wait_warp(d_full + 8 * dbuf, dph, s_abort, nullptr);
+        if (!alive) break;
+        tc_fence_after();
+        for (int q = copies - 1; q >= 0; --q) {                // the smallest pieces first
+          const uint32_t from = taddr + dbuf * p.rows + q * p.Mt;
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 16) {
+            if (c0 >= p.Mt) break;
+            uint32_t v[16];
+            tmem_ld16(from + c0, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[c0 + j] += __uint_as_float(v[j]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(d_empty + 8 * dbuf);
+      }
+      // the rings are free once the last sums are complete: every copy has landed and been read
+#pragma unroll
+      for (int c0 = 0; c0 < 128; c0 += 16) {
+        if (c0 >= p.Mt) break;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sums[(c0 + j) * 128] = acc[c0 + j];
+      }
+    } else {
+      if (supers > 0) alive = mbar_wait_warp(d_full, 0, s_abort, nullptr);
+      tc_fence_after();
+      for (int c0 = 0; c0 < p.Mt; c0 += 8) {
+        float f[8] = {};
+        if (supers > 0 && alive) {
+          for (int q = copies - 1; q >= 0; --q) {
+            uint32_t v[8];
+            tmem_ld8(taddr + q * p.Mt + c0, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(v[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[(c0 + j) * 128] = f[j];
+      }
+    }
+  }
+
+  // ---- sums of the cluster -> y, a row of 128 channels per warp -------------------------------------
+  tc_fence_before();
+  __syncthreads();
+  if (*s_abort) {                                  // a wait that ran out shows in the result
+    for (int i = tid; i < p.Mt * 128; i += kMxTcThreads) reinterpret_cast<float*>(smem)[i] = __int_as_float(0x7FC00000);
+    __syncthreads();
+  }
+  if (p.cluster > 1) {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
+  }
+  if (KIND == 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int rows = min(p.Mt, p.M - m0);
+  for (int r = rank + warp * p.cluster; r < rows; r += (kMxTcThreads / 32) * p.cluster) {
+    T* dst = y + (int64_t)(m0 + r) * y_stride + n0;
+    if (vec) {                                                 // rows of y start on four values: a lane takes four channels
+      float4 v = *reinterpret_cast<const float4*>(s_bias + lane * 4);
+      const uint32_t mine = smem_u32(smem) + (uint32_t)(r * 128 + lane * 4) * 4;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int q = 0; q < p.cluster; ++q) {
+        uint32_t theirs;
+        float4 part;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(theirs) : "r"(mine), "r"(q));
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(part.x), "=f"(part.y), "=f"(part.z), "=f"(part.w) : "r"(theirs) : "memory");
+        sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
+      }
+      v.x += sum.x; v.y += sum.y; v.z += sum.z; v.w += sum.w;
+      if (n0 + lane * 4 + 4 <= p.N) {
+        if (sizeof(T) == 4) {
+          *reinterpret_cast<float4*>(dst + lane * 4) = v;
+        } else {
+          T h[4] = {from_float<T>(v.x), from_float<T>(v.y), from_float<T>(v.z), from_float<T>(v.w)};
+          *reinterpret_cast<uint2*>(dst + lane * 4) = *reinterpret_cast<const uint2*>(h);
+        }
+        continue;
+      }
+      const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n0 + lane * 4 + j < p.N) dst[lane * 4 + j] = from_float<T>(f[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int ch = lane + 32 * j;
+        const uint32_t mine = smem_u32(smem) + (uint32_t)(r * 128 + ch) * 4;
+        float sum = 0.f;
+        for (int q = 0; q < p.cluster; ++q) {
+          uint32_t theirs;
+          float part;
+          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(theirs) : "r"(mine), "r"(q));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(theirs) : "memory");
+          sum += part;
+        }
+        if (n0 + ch < p.N) dst[ch] = from_float<T>(sum + s_bias[ch]);
+      }
+    }
+  }
+  if (p.cluster > 1) {                                         // no CTA leaves while another reads its sums
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// x -> eight-bit pieces
+// ---------------------------------------------------------------------------------------
+constexpr int kSplitThreads = 256;
+
+// A lane takes eight values, four lanes a block.  Piece 0 is the values times the power of two that brings the block's largest
+// into [128, 256), rounded to four bits; what is left, at most 2^-5 of the unit above, times 32, is the next piece's input.
+template <typename T, int PIECES>
+__global__ void __launch_bounds__(kSplitThreads)
+mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int M, int vec, FastDiv words, int scale_row, uint64_t units,
+                  uint2* __restrict__ planes, uint8_t* __restrict__ scales) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint64_t u = (uint64_t)blockIdx.x * kSplitThreads + threadIdx.x;
+  const bool live = u < units;
+  const uint32_t row = live ? (uint32_t)(u < (1ull << 31) ? words.div((uint32_t)u) : u / words.d) : 0u;
+  const uint32_t word = live ? (uint32_t)(u - (uint64_t)row * words.d) : 0u;
+  const int k = (int)word * 8;
+  const T* src = x + (int64_t)row * x_stride + k;
+  float f[8];
+  if (vec && live && k + 8 <= K) {
+    load8(src, f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = live && k + j < K ? to_float(src[j]) : 0.f;
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  if (!live) return;
+  const uint32_t e = top >> 23;
+  const bool dead = e == 255;
+  uint32_t s = dead ? 255u : e < 7 ? 0u : e - 7;
+  float up = mx_inverse_scale(s);
+  uint8_t* sr = scales + (int64_t)row * scale_row;
+  const int64_t piece_words = (int64_t)M * words.d, piece_scales = (int64_t)M * scale_row;
+#pragma unroll
+  for (int q = 0; q < PIECES; ++q) {
+    uint32_t out[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = f[2 * j] * up, b = f[2 * j + 1] * up;
+      uint16_t c;
+      uint32_t back;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(b), "f"(a));
+      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(c));
+      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&back));
+      f[2 * j] = a - v.x;
+      f[2 * j + 1] = b - v.y;
+      out[j >> 1] |= (uint32_t)c << ((j & 1) * 16);
+    }
+    planes[q * piece_words + u] = dead ? make_uint2(0u, 0u) : make_uint2(out[0], out[1]);
+    if ((word & 3) == 0) sr[q * piece_scales + (word >> 2)] = (uint8_t)s;
+    if (word + 1 == words.d)
+      for (int b = (int)words.d / 4; b < scale_row; ++b) sr[q * piece_scales + b] = 0;
+    if (!dead) {
+      const uint32_t next = s < 5 ? 0u : s - 5;
+      up = (float)(1u << (s - next));
+      s = next;
+    }
+  }
+}
+
+inline int mx_pieces(int dtype) { return dtype == AIQ_DTYPE_F32 ? 5 : dtype == AIQ_DTYPE_F16 ? 3 : 2; }
+inline int64_t mx_plane_row(int K) { return ((int64_t)K + 127) / 128 * 128; }
+
+template <typename T, int PIECES>
+aiq_status_t split_x(const MxProduct& p, uint8_t* planes, uint8_t* scales, cudaStream_t s) {
+  const uint32_t words = (uint32_t)(mx_plane_row(p.K) / 8);
+  const uint64_t units = (uint64_t)p.M * words;
+  const int vec = (((uintptr_t)p.x) & 15) == 0 && (p.M == 1 || p.x_stride * (int64_t)sizeof(T) % 16 == 0);
+  mx_split_x_kernel<T, PIECES><<<(unsigned)((units + kSplitThreads - 1) / kSplitThreads), kSplitThreads, 0, s>>>(
+      static_cast<const T*>(p.x), p.x_stride, p.K, p.M, vec, FastDiv(words), (int)mx_scale_row_bytes(p.K), units,
+      reinterpret_cast<uint2*>(planes), scales);
+  AIQ_LAUNCH_CHECK("mx_split_x");
+  return AIQ_OK;
+}
+
+aiq_status_t encode(EncodeTiledFn enc, CUtensorMap* map, CUtensorMapDataType type, const void* base, int rank, const cuuint64_t* dims,
+                    const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
+  const cuuint32_t ones[3] = {1, 1, 1};
+  const CUresult r = enc(map, type, rank, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? AIQ_OK : set_error(AIQ_ERR_CUDA, "cuTensorMapEncodeTiled (microscaled product) failed with code %d", (int)r);
+}
+
+template <int KIND, typename T>
+aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s) {
+  using Kd = MxKind<KIND>;
+  constexpr bool PROMOTE = sizeof(T) == 4;
+  DeviceProps props;
+  if (aiq_status_t st = current_device_props(&props)) return st;
+  AIQ_ENSURE_DYNAMIC_SMEM((mx_tc_kernel<KIND, T>), props.smem_optin);
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return set_error(AIQ_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+
+  MxTcParams p = {};
+  p.N = g.N; p.M = g.M;
+  p.pieces = KIND == 1 ? mx_pieces(g.dtype) : 1;
+  p.n_chunks = (g.K + Kd::CHUNK - 1) / Kd::CHUNK;
+  const int n_super = (g.K + kMxSuper - 1) / kMxSuper, row_blocks = (g.N + 127) / 128;
+  // rows of x per tile: the sums of a tile and the scale words have to fit into 512 columns
+  const int widest = PROMOTE ? 128 : 256, stacked = p.pieces == 1 ? widest : (PROMOTE ? 160 : 256) / p.pieces / 16 * 16;
+  p.stack = g.M <= stacked;
+  const int most = p.stack ? stacked : widest;
+  p.Mt = g.M >= most ? most : (g.M + 15) / 16 * 16;
+  p.rows = p.stack ? p.Mt * p.pieces : p.Mt;
+  p.b_cols = ((p.rows + 31) / 32 + 3) / 4 * 4;
+  p.sf_group = 4 + p.b_cols * (p.stack ? 1 : p.pieces);
+  p.sf_col = PROMOTE ? 2 * p.rows : p.rows;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < p.sf_col + 8 * p.sf_group) p.tmem_cols <<= 1;
+  if (p.tmem_cols > 512) return set_error(AIQ_ERR_SHAPE, "mx_tc: %d columns of tensor memory", p.tmem_cols);
+  const int m_blocks = (g.M + p.Mt - 1) / p.Mt;
+  int splits = props.n_sms / (row_blocks * m_blocks);
+  p.cluster = 1;
+  while (p.cluster * 2 <= splits && p.cluster * 2 <= n_super && p.cluster < 8) p.cluster *= 2;
+  p.supers_per_split = (n_super + p.cluster - 1) / p.cluster;
+  const int chunks = p.supers_per_split * Kd::CPS, units = p.stack ? 1 : p.pieces;
+  p.a_stages = units > 1 ? Kd::CPS : 2;                        // the pieces of one set of chunks read the same weights
+  p.b_stages = 2;
+  auto fits = [&](int a, int b) { MxTcParams t = p; t.a_stages = a; t.b_stages = b; return mx_smem_bytes(t) <= props.smem_optin; };
+  if (!fits(p.a_stages, p.b_stages)) return set_error(AIQ_ERR_SHAPE, "mx_tc: %d bytes of shared memory", mx_smem_bytes(p));
+  for (bool more = true; more;) {
+    const bool a_can = p.a_stages < kMxMaxStages && p.a_stages < chunks && fits(p.a_stages + 1, p.b_stages);
+    const bool b_can = p.b_stages < kMxMaxStages * 2 && p.b_stages < chunks * units && fits(p.a_stages, p.b_stages + 1);
+    if (a_can && (p.a_stages * units <= p.b_stages || !b_can)) ++p.a_stages;
+    else if (b_can) ++p.b_stages;
+    else more = false;
+  }
+
+  const cuuint64_t w_row = (cuuint64_t)mx_row_bytes(g.K), s_row = (cuuint64_t)mx_scale_row_bytes(g.K), N = g.N, M = g.M;
+  CUtensorMap a_map, b_map, sa_map, sb_map;
+  {
+    const cuuint64_t dims[2] = {KIND == 0 ? w_row : 2 * w_row, N}, strides[1] = {w_row};
+    const cuuint32_t box[2] = {128, 128};
+    if (aiq_status_t st = encode(enc, &a_map, KIND == 0 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, g.w_codes, 2,
+                                 dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
+    const cuuint64_t sdims[2] = {s_row, N}, sstrides[1] = {s_row};
+    const cuuint32_t sbox[2] = {16, 128};
+    if (aiq_status_t st = encode(enc, &sa_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.w_scales, 2, sdims, sstrides, sbox, CU_TENSOR_MAP_SWIZZLE_NONE))
+      return st;
+  }
+  {
+    const cuuint64_t x_row = KIND == 0 ? w_row : (cuuint64_t)mx_plane_row(g.K), P = p.pieces;
+    const uint8_t* codes = KIND == 0 ? g.x_codes : workspace;
+    const uint8_t* scales = KIND == 0 ? g.x_scales : workspace + P * M * x_row;
+    const cuuint64_t dims[3] = {x_row, M, P}, strides[2] = {x_row, x_row * M};
+    const cuuint32_t box[3] = {128, (cuuint32_t)p.Mt, (cuuint32_t)(p.stack ? P : 1)};
+    if (aiq_status_t st = encode(enc, &b_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
+    const cuuint64_t sdims[3] = {s_row, M, P}, sstrides[2] = {s_row, s_row * M};
+    const cuuint32_t sbox[3] = {16, (cuuint32_t)p.Mt, (cuuint32_t)(p.stack ? P : 1)};
+    if (aiq_status_t st = encode(enc, &sb_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, 3, sdims, sstrides, sbox, CU_TENSOR_MAP_SWIZZLE_NONE))
+      return st;
+  }
+  const int y_step = 4 * (int)sizeof(T);                       // bytes a lane writes
+  const int vec = (((uintptr_t)g.y) % y_step) == 0 && (g.M == 1 || g.y_stride * (int64_t)sizeof(T) % y_step == 0);
+  LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * g.M * g.N * g.K,
+                    (double)(g.N + (KIND == 0 ? g.M : 0)) * (w_row + s_row) + sizeof(T) * (double)g.M * (g.N + (KIND == 1 ? g.K : 0)));
+  if (KIND == 1) {
+    uint8_t* scales = workspace + (size_t)p.pieces * M * mx_plane_row(g.K);
+    aiq_status_t st = AIQ_OK;
+    if (sizeof(T) == 4) st = split_x<T, 5>(g, workspace, scales, s);
+    else if (g.dtype == AIQ_DTYPE_F16) st = split_x<T, 3>(g, workspace, scales, s);
+    else st = split_x<T, 2>(g, workspace, scales, s);
+    if (st != AIQ_OK) return st;
+  }
+  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T>, dim3(row_blocks * p.cluster, m_blocks), dim3(kMxTcThreads),
+                                      (size_t)mx_smem_bytes(p), s, a_map, b_map, sa_map, sb_map, p, g.bias, static_cast<T*>(g.y), g.y_stride, vec));
+  AIQ_LAUNCH_CHECK("mx_tc");
+  return AIQ_OK;
+}
+
+}  // namespace
+
+size_t mx_tc_workspace_bytes(int K, int M, int dtype) {
+  return align_up((size_t)mx_pieces(dtype) * M * (size_t)(mx_plane_row(K) + mx_scale_row_bytes(K)), 16);
+}
+
+aiq_status_t launch_mx_product_tc(const MxProduct& p, void* workspace, cudaStream_t s) {
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (p.x) {
+    switch (p.dtype) {
+      case AIQ_DTYPE_F32: return launch_kind<1, float>(p, ws, s);
+      case AIQ_DTYPE_F16: return launch_kind<1, __half>(p, ws, s);
+      default: return launch_kind<1, __nv_bfloat16>(p, ws, s);
+    }
+  }
+  switch (p.dtype) {
+    case AIQ_DTYPE_F32: return launch_kind<0, float>(p, ws, s);
+    case AIQ_DTYPE_F16: return launch_kind<0, __half>(p, ws, s);
+    default: return launch_kind<0, __nv_bfloat16>(p, ws, s);
+  }
+}
+
+}  // namespace aiq
