@@ -267,41 +267,85 @@ def _dtype(dtype):
     return code
 
 
+# Shapes, strides and types decide all that the checks below look at; their answers are kept for the next call with the same ones
+# (a check takes as long as a kernel launch).  What else can differ is looked at every time.
+def _mx_plan(key, check, *args):
+    plan = check(*args)
+    if len(_mx_plans) >= 4096:
+        _mx_plans.clear()
+    _mx_plans[key] = plan
+    return plan
+
+
+_mx_plans = {}
+
+
+def _mx_stream(stream, *tensors):
+    """The launch goes to the current device (its current stream): every tensor has to lie there."""
+    if _raw_stream is None:
+        _stream()
+    current, raw = _raw_stream
+    device = current()
+    for t in tensors:                                   # -1: not a CUDA tensor
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"expected every tensor on the current device, cuda:{device}, not {t.device}")
+    return raw(device) if stream is None else stream.cuda_stream
+
+
 def _mx_rows(t):
-    """(pointer, type, rows, K, row stride) of a CUDA matrix whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 2:
-        raise ValueError("expected a CUDA matrix")
+    """(type, rows, K, row stride) of a matrix whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError(f"expected a matrix, not {tuple(t.shape)}")
     rows, k = t.shape
     stride, step = t.stride()
     if step != 1 and k != 1:
         raise ValueError("expected contiguous rows")
-    return t.data_ptr(), _dtype(t.dtype), rows, k, stride
+    return _dtype(t.dtype), rows, k, stride
 
 
 def _mx_held(codes, scales, k):
-    """(codes pointer, scales pointer, rows) of microscaled rows of k values."""
-    c, s = _dev(codes), _dev(scales)
+    """The rows of k values each that codes and scales hold."""
+    if not codes.is_cuda or not scales.is_cuda:
+        raise ValueError("expected CUDA tensors")
     rows = codes.shape[0]
-    if tuple(codes.shape) != (rows, (k + 127) // 128 * 64) or tuple(scales.shape) != (rows, (k + 511) // 512 * 16) \
-            or codes.element_size() != 1 or scales.element_size() != 1:
-        raise ValueError(f"expected codes [{rows}][{(k + 127) // 128 * 64}] and scales [{rows}][{(k + 511) // 512 * 16}] in bytes "
-                         f"for rows of {k} values, not {tuple(codes.shape)} and {tuple(scales.shape)}")
-    return c, s, rows
+    want = (rows, (k + 127) // 128 * 64), (rows, (k + 511) // 512 * 16)
+    if (tuple(codes.shape), tuple(scales.shape)) != want or codes.element_size() != 1 or scales.element_size() != 1:
+        raise ValueError(f"expected codes and scales of bytes, {want[0]} and {want[1]} for rows of {k} values, not {tuple(codes.shape)} and "
+                         f"{tuple(scales.shape)}")
+    if not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("expected contiguous codes and scales")
+    return rows
 
 
 def _mx_bias(bias, n):
-    if bias is not None and (bias.numel() != n or bias.element_size() != 4 or not bias.is_floating_point()):
-        raise ValueError(f"expected a float32 bias of {n} values")
-    return _dev(bias)
+    if bias is not None and (bias.numel() != n or bias.element_size() != 4 or not bias.is_floating_point() or not bias.is_contiguous()):
+        raise ValueError(f"expected a contiguous float32 bias of {n} values")
 
 
-def _mx_device(*tensors):
-    """The launch goes to the current device's stream: every tensor has to lie there."""
-    import torch
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"expected every tensor on the current device, cuda:{device}, not {t.device}")
+def _mx_check_values(codes, scales, values):
+    dtype, rows, k, stride = _mx_rows(values)
+    if _mx_held(codes, scales, k) != rows:
+        raise ValueError(f"codes of {codes.shape[0]} rows and {rows} rows of values")
+    return dtype, rows, k, stride
+
+
+def _mx_check_linear(codes, scales, bias, x, y):
+    dtype, m, k, x_stride = _mx_rows(x)
+    y_dtype, y_rows, n, y_stride = _mx_rows(y)
+    held = _mx_held(codes, scales, k)
+    if (y_dtype, y_rows, held) != (dtype, m, n):
+        raise ValueError(f"x {tuple(x.shape)} {x.dtype}, weights of {held} rows and y {tuple(y.shape)} {y.dtype} do not match")
+    _mx_bias(bias, n)
+    return n, k, dtype, m, x_stride, y_stride
+
+
+def _mx_check_matmul(a_codes, a_scales, b_codes, b_scales, bias, y, K):
+    dtype, m, n, y_stride = _mx_rows(y)
+    rows = _mx_held(a_codes, a_scales, K), _mx_held(b_codes, b_scales, K)
+    if rows != (m, n):
+        raise ValueError(f"A of {rows[0]} rows, B of {rows[1]} and y {tuple(y.shape)} do not match")
+    _mx_bias(bias, n)
+    return m, n, dtype, y_stride
 
 
 def aiq_mx_row_bytes(K):
@@ -315,22 +359,23 @@ def aiq_mx_scale_row_bytes(K):
 def aiq_mx_quantize(x, codes_out, scales_out, stream=None):
     """x [rows][K] float32, float16 or bfloat16 (rows may have any stride) -> codes_out uint8 [rows][aiq_mx_row_bytes(K)],
     scales_out uint8 [rows][aiq_mx_scale_row_bytes(K)]."""
-    ptr, dtype, rows, k, stride = _mx_rows(x)
-    c, s, held = _mx_held(codes_out, scales_out, k)
-    if held != rows:
-        raise ValueError(f"{rows} rows into codes of {held}")
-    _mx_device(x, codes_out, scales_out)
-    _check(lib.aiq_mx_quantize(ptr, dtype, rows, k, stride, c, s, _stream(stream)))
+    key = (codes_out.shape, scales_out.shape, x.shape, x.stride(), x.dtype, codes_out.dtype, scales_out.dtype,
+           codes_out.is_contiguous(), scales_out.is_contiguous())
+    dtype, rows, k, stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_values, codes_out, scales_out, x)
+    s = _mx_stream(stream, x, codes_out, scales_out)
+    status = lib.aiq_mx_quantize(x.data_ptr(), dtype, rows, k, stride, codes_out.data_ptr(), scales_out.data_ptr(), s)
+    if status:
+        _check(status)
 
 
 def aiq_mx_dequantize(codes, scales, y, stream=None):
     """codes, scales -> y [rows][K] float32, float16 or bfloat16."""
-    ptr, dtype, rows, k, stride = _mx_rows(y)
-    c, s, held = _mx_held(codes, scales, k)
-    if held != rows:
-        raise ValueError(f"codes of {held} rows into {rows}")
-    _mx_device(y, codes, scales)
-    _check(lib.aiq_mx_dequantize(c, s, rows, k, dtype, ptr, stride, _stream(stream)))
+    key = (codes.shape, scales.shape, y.shape, y.stride(), y.dtype, codes.dtype, scales.dtype, codes.is_contiguous(), scales.is_contiguous())
+    dtype, rows, k, stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_values, codes, scales, y)
+    s = _mx_stream(stream, y, codes, scales)
+    status = lib.aiq_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, dtype, y.data_ptr(), stride, s)
+    if status:
+        _check(status)
 
 
 def aiq_mx_linear_workspace_bytes(N, K, M, dtype):
@@ -339,27 +384,26 @@ def aiq_mx_linear_workspace_bytes(N, K, M, dtype):
 
 def aiq_mx_linear(codes, scales, bias, x, y, workspace=None, stream=None):
     """y [M][N] = x [M][K] * W^T + bias; W [N][K] as codes and scales, x and y of one type, bias float32 [N] or None."""
-    xp, dtype, m, k, x_stride = _mx_rows(x)
-    yp, y_dtype, y_rows, n, y_stride = _mx_rows(y)
-    c, s, held = _mx_held(codes, scales, k)
-    if (y_dtype, y_rows, held) != (dtype, m, n):
-        raise ValueError(f"x {tuple(x.shape)} {x.dtype}, weights of {held} rows and y {tuple(y.shape)} {y.dtype} do not match")
-    _mx_device(x, y, codes, scales, bias, workspace)
-    status = lib.aiq_mx_linear(c, s, _mx_bias(bias, n), n, k, xp, dtype, m, x_stride, yp, y_stride, _dev(workspace),
-                               workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream(stream))
+    key = (codes.shape, scales.shape, x.shape, y.shape, x.stride(), y.stride(), x.dtype, y.dtype, codes.dtype, scales.dtype,
+           codes.is_contiguous(), scales.is_contiguous(), (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None)
+    n, k, dtype, m, x_stride, y_stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_linear, codes, scales, bias, x, y)
+    s = _mx_stream(stream, x, y, codes, scales, bias, workspace)
+    ws, size = (_dev(workspace), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
+    status = lib.aiq_mx_linear(codes.data_ptr(), scales.data_ptr(), bias.data_ptr() if bias is not None else None, n, k, x.data_ptr(), dtype,
+                               m, x_stride, y.data_ptr(), y_stride, ws, size, s)
     if status:
         _check(status)
 
 
 def aiq_mx_matmul(a_codes, a_scales, b_codes, b_scales, bias, K, y, stream=None):
     """y [M][N] = A [M][K] * B [N][K]^T + bias; both matrices as codes and scales, y float32, float16 or bfloat16."""
-    yp, dtype, m, n, y_stride = _mx_rows(y)
-    ac, as_, a_rows = _mx_held(a_codes, a_scales, K)
-    bc, bs, b_rows = _mx_held(b_codes, b_scales, K)
-    if (a_rows, b_rows) != (m, n):
-        raise ValueError(f"A of {a_rows} rows, B of {b_rows} and y {tuple(y.shape)} do not match")
-    _mx_device(y, a_codes, a_scales, b_codes, b_scales, bias)
-    status = lib.aiq_mx_matmul(ac, as_, m, bc, bs, n, _mx_bias(bias, n), int(K), yp, dtype, y_stride, _stream(stream))
+    key = (K, a_codes.shape, a_scales.shape, b_codes.shape, b_scales.shape, y.shape, y.stride(), y.dtype, a_codes.dtype, a_scales.dtype,
+           b_codes.dtype, b_scales.dtype, a_codes.is_contiguous(), a_scales.is_contiguous(), b_codes.is_contiguous(),
+           b_scales.is_contiguous(), (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None)
+    m, n, dtype, y_stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_matmul, a_codes, a_scales, b_codes, b_scales, bias, y, int(K))
+    s = _mx_stream(stream, y, a_codes, a_scales, b_codes, b_scales, bias)
+    status = lib.aiq_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), m, b_codes.data_ptr(), b_scales.data_ptr(), n,
+                               bias.data_ptr() if bias is not None else None, int(K), y.data_ptr(), dtype, y_stride, s)
     if status:
         _check(status)
 

@@ -1,5 +1,6 @@
 // Microscaled 4-bit floating point: quantizing, expanding, and the product for any shape; see mx.cuh for the format.
 #include "mx.cuh"
+#include "tc_ptx.cuh"
 
 namespace aiq {
 namespace {
@@ -229,101 +230,168 @@ aiq_status_t dequantize_rows(const uint8_t* codes, const uint8_t* scales, int64_
 }
 
 // ---------------------------------------------------------------------------------------
-// the product, any shape
+// the product, any shape; the kernel for a few rows of x and for small matrices
 // ---------------------------------------------------------------------------------------
-// A warp computes one output channel for MT rows of x; a lane takes every 32nd block of the weight row.  float32 throughout.
-constexpr int kPlainRows = 4;
+// A warp computes R output channels for MT rows of x, or a share of their k.  A lane takes a word of eight codes at a time, so that
+// the loads of a warp are whole lines: 128 bytes of codes, and the 256 values of x that belong to them.  All loads of U words are
+// under way before the first is used.  float32 throughout, two products per instruction.
+constexpr int kRowChannels = 2;
 
-// eight values of x from k on (k a multiple of 8)
+// eight values of x from k on (k a multiple of 8), as they are loaded and as floats; zero behind K
 template <typename T>
-struct PlainX {
-  static constexpr bool kScaled = false;
+struct RowsOf {
+  struct Raw { uint4 v[sizeof(T) / 2]; };
   const T* x;
   int64_t stride;
   bool vec;
-  __device__ __forceinline__ float block_scale(int64_t, int) const { return 1.f; }
-  __device__ __forceinline__ void get8(int64_t m, int k, int K, float* f) const {
+  __device__ __forceinline__ Raw get(int64_t m, int k, int K) const {
     const T* p = x + m * stride + k;
+    Raw r;
     if (vec && k + 8 <= K) {
-      load8(p, f);
-    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = k + j < K ? to_float(p[j]) : 0.f;
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+    } else {
+      T v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = k + j < K ? p[j] : from_float<T>(0.f);
+      memcpy(&r, v, sizeof(r));
     }
+    return r;
+  }
+  static __device__ __forceinline__ Raw none() { return Raw{}; }
+  static __device__ __forceinline__ void values(const Raw& r, float* f) {
+    T v[8];
+    memcpy(v, &r, sizeof(r));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = to_float(v[j]);
   }
 };
-struct PlainMx {
-  static constexpr bool kScaled = true;
+struct RowsHeld {
+  struct Raw { uint32_t codes, scale; };
   const uint8_t *codes, *scales;
   int64_t row_bytes, scale_row;
-  __device__ __forceinline__ float block_scale(int64_t m, int b) const { return mx_scale(scales[m * scale_row + b]); }
-  __device__ __forceinline__ void get8(int64_t m, int k, int, float* f) const {
-    mx_expand8(*reinterpret_cast<const uint32_t*>(codes + m * row_bytes + (k >> 1)), f);
+  __device__ __forceinline__ Raw get(int64_t m, int k, int) const {
+    return Raw{*reinterpret_cast<const uint32_t*>(codes + m * row_bytes + (k >> 1)), scales[m * scale_row + (k >> 5)]};
+  }
+  static __device__ __forceinline__ Raw none() { return Raw{0u, 0u}; }
+  static __device__ __forceinline__ void values(const Raw& r, float* f) {
+    mx_expand8(r.codes, f);
+    const float s = mx_scale(r.scale);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] *= s;
   }
 };
 
-template <typename X, typename T>
+template <typename X, typename T, int MT, int U>
 __global__ void __launch_bounds__(kMxThreads)
-mx_product_plain_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t row_bytes, int64_t scale_row,
-                        const float* __restrict__ bias, int N, int K, int M, T* __restrict__ y, int64_t y_stride) {
-  const int n = blockIdx.x * (kMxThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (n >= N) return;
-  const int blocks = (K + MX_BLOCK - 1) / MX_BLOCK;
-  for (int64_t m0 = (int64_t)blockIdx.y * kPlainRows; m0 < M; m0 += (int64_t)gridDim.y * kPlainRows) {
-    float acc[kPlainRows] = {};
-    for (int b = lane; b < blocks; b += 32) {
-      const uint4 raw = *reinterpret_cast<const uint4*>(codes + n * row_bytes + (int64_t)b * 16);
-      const float ws = mx_scale(scales[n * scale_row + b]);
-      const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-      float sum[kPlainRows] = {};
+mx_product_rows_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t row_bytes, int64_t scale_row,
+                       const float* __restrict__ bias, int N, int K, int M, int k_warps, T* __restrict__ y, int64_t y_stride) {
+  constexpr int R = kRowChannels, WARPS = kMxThreads / 32;
+  __shared__ float part[WARPS][R * MT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kw = warp % k_warps;
+  const int n0 = (blockIdx.x * (WARPS / k_warps) + warp / k_warps) * R;
+  const int words = (K + 7) / 8;
+  for (int64_t m0 = (int64_t)blockIdx.y * MT; m0 < M; m0 += (int64_t)gridDim.y * MT) {
+    uint64_t acc[R][MT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float wf[8], xf[8];
-        mx_expand8(w[j], wf);
-        if (!X::kScaled) {                       // the weights' own values: x may be as large as its type allows
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) wf[e] *= ws;
+      for (int r = 0; r < MT; ++r) acc[i][r] = 0;
+    for (int w0 = kw * 32 * U + lane; w0 - lane < words && n0 < N; w0 += k_warps * 32 * U) {
+      uint32_t raw[R][U], sb[R][U];
+      typename X::Raw xr[MT][U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int w = w0 + u * 32;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const bool live = w < words && n0 + i < N;
+          raw[i][u] = live ? *reinterpret_cast<const uint32_t*>(codes + (n0 + i) * row_bytes + (int64_t)w * 4) : 0u;
+          sb[i][u] = live ? scales[(n0 + i) * scale_row + (w >> 2)] : 0u;
         }
 #pragma unroll
-        for (int r = 0; r < kPlainRows; ++r) {
-          if (m0 + r < M) {
-            x.get8(m0 + r, b * MX_BLOCK + j * 8, K, xf);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[r] = fmaf(wf[e], xf[e], sum[r]);
-          }
+        for (int r = 0; r < MT; ++r) {
+          if (w < words && m0 + r < M) xr[r][u] = x.get(m0 + r, w * 8, K);
+          else xr[r][u] = X::none();
         }
       }
 #pragma unroll
-      for (int r = 0; r < kPlainRows; ++r)
-        if (m0 + r < M) acc[r] = X::kScaled ? fmaf(sum[r], x.block_scale(m0 + r, b) * ws, acc[r]) : acc[r] + sum[r];
+      for (int u = 0; u < U; ++u) {
+        uint64_t wf[R][4];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          float f[8];
+          mx_expand8(raw[i][u], f);
+          const float s = mx_scale(sb[i][u]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) wf[i][j] = mul2(pack2(f[2 * j], f[2 * j + 1]), pack2(s, s));
+        }
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+          float f[8];
+          X::values(xr[r][u], f);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint64_t v = pack2(f[2 * j], f[2 * j + 1]);
+#pragma unroll
+            for (int i = 0; i < R; ++i) acc[i][r] = fma2(wf[i][j], v, acc[i][r]);
+          }
+        }
+      }
     }
 #pragma unroll
-    for (int r = 0; r < kPlainRows; ++r) {
+    for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
-      if (lane == 0 && m0 + r < M) y[(m0 + r) * y_stride + n] = from_float<T>(acc[r] + (bias ? bias[n] : 0.f));
+      for (int r = 0; r < MT; ++r) {
+        const float2 a = unpack2(acc[i][r]);
+        float v = a.x + a.y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0) part[warp][i * MT + r] = v;
+      }
+    if (k_warps > 1) __syncthreads(); else __syncwarp();
+    if (kw == 0 && lane < R * MT) {
+      const int i = lane / MT, r = lane % MT;
+      float v = 0.f;
+      for (int k = 0; k < k_warps; ++k) v += part[warp + k][lane];
+      if (n0 + i < N && m0 + r < M) y[(m0 + r) * y_stride + n0 + i] = from_float<T>(v + (bias ? bias[n0 + i] : 0.f));
     }
+    if (k_warps > 1) __syncthreads(); else __syncwarp();
   }
 }
 
-template <typename T>
-aiq_status_t product_plain(const MxProduct& p, cudaStream_t s) {
+template <int MT, int U, typename X, typename T>
+aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
   const int64_t row_bytes = mx_row_bytes(p.K), scale_row = mx_scale_row_bytes(p.K);
-  const dim3 grid((p.N + kMxThreads / 32 - 1) / (kMxThreads / 32), min((p.M + kPlainRows - 1) / kPlainRows, 65535));
+  // Warps along k until a warp's share is one round of loads, as long as that gives blocks to SMs without: one row, 4096 x 4096, 12.0 us
+  // with 148 blocks at most, 9.9 with 296, 9.2 with 592 and more; 8192 x 8192 31.1, 31.1, 28.0, without a limit 30.7.
+  int k_warps = 1;
+  const int64_t m_blocks = (p.M + MT - 1) / MT;
+  while (k_warps < kMxThreads / 32 && k_warps * 256 * U < p.K && (int64_t)p.N * k_warps / (kMxThreads / 32 * kRowChannels) * m_blocks < 592)
+    k_warps *= 2;
+  const int per_block = kMxThreads / 32 / k_warps * kRowChannels;
+  const dim3 grid((p.N + per_block - 1) / per_block, min((p.M + MT - 1) / MT, 65535));
+  mx_product_rows_kernel<X, T, MT, U><<<grid, kMxThreads, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N, p.K, p.M,
+                                                                 k_warps, static_cast<T*>(p.y), p.y_stride);
+  AIQ_LAUNCH_CHECK("mx_product_rows");
+  return AIQ_OK;
+}
+template <typename X, typename T>
+aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
   LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * p.M * p.N * p.K,
-                    (double)(p.N + (p.x ? 0 : p.M)) * (row_bytes + scale_row) + sizeof(T) * (double)p.M * (p.N + (p.x ? p.K : 0)));
+                    (double)(p.N + (p.x ? 0 : p.M)) * (mx_row_bytes(p.K) + mx_scale_row_bytes(p.K)) + sizeof(T) * (double)p.M * (p.N + (p.x ? p.K : 0)));
+  if (p.M == 1) return product_rows<1, 4, X, T>(p, x, s);
+  if (p.M == 2) return product_rows<2, 2, X, T>(p, x, s);
+  return product_rows<4, 2, X, T>(p, x, s);
+}
+
+template <typename T>
+aiq_status_t product_rows(const MxProduct& p, cudaStream_t s) {
   if (p.x) {
     const bool vec = (((uintptr_t)p.x) & 15) == 0 && (p.M == 1 || p.x_stride * (int64_t)sizeof(T) % 16 == 0);
-    const PlainX<T> x = {static_cast<const T*>(p.x), p.x_stride, vec};
-    mx_product_plain_kernel<<<grid, kMxThreads, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N, p.K, p.M,
-                                                        static_cast<T*>(p.y), p.y_stride);
-  } else {
-    const PlainMx x = {p.x_codes, p.x_scales, row_bytes, scale_row};
-    mx_product_plain_kernel<<<grid, kMxThreads, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N, p.K, p.M,
-                                                        static_cast<T*>(p.y), p.y_stride);
+    return product_rows<RowsOf<T>, T>(p, RowsOf<T>{static_cast<const T*>(p.x), p.x_stride, vec}, s);
   }
-  AIQ_LAUNCH_CHECK("mx_product_plain");
-  return AIQ_OK;
+  return product_rows<RowsHeld, T>(p, RowsHeld{p.x_codes, p.x_scales, mx_row_bytes(p.K), mx_scale_row_bytes(p.K)}, s);
 }
 
 }  // namespace
@@ -346,11 +414,11 @@ aiq_status_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, i
   }
 }
 
-aiq_status_t launch_mx_product_plain(const MxProduct& p, cudaStream_t s) {
+aiq_status_t launch_mx_product_rows(const MxProduct& p, cudaStream_t s) {
   switch (p.dtype) {
-    case AIQ_DTYPE_F32: return product_plain<float>(p, s);
-    case AIQ_DTYPE_F16: return product_plain<__half>(p, s);
-    default: return product_plain<__nv_bfloat16>(p, s);
+    case AIQ_DTYPE_F32: return product_rows<float>(p, s);
+    case AIQ_DTYPE_F16: return product_rows<__half>(p, s);
+    default: return product_rows<__nv_bfloat16>(p, s);
   }
 }
 
@@ -407,9 +475,16 @@ extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales,
                                    (cudaStream_t)stream);
 }
 
+// Whether the kernel for few rows and small matrices beats the tensor-core kernel, whose time below 2^22 products is its chain of
+// set-up, first loads and last stores.  On the device, rows | tensor cores (linear layer: with its pre-pass, a second launch):
+//   linear, bf16     1 row: 1280 x 320 2.6 | 7.0 us, 2000 x 2000 4.7 | 8.2, 4096 x 4096 9.2 | 9.7, 8192 x 8192 28 | 15.5
+//                    4 rows: 724 x 724 4.9 | 7.5, 2000 x 2000 8.4 | 8.2;  8 rows, 724 x 724 5.6 | 7.4;  16 rows 9.4 | 7.6
+//   both microscaled 1 row: 2000 x 2000 4.8 | 6.3, 4096 x 4096 10.0 | 7.6;  8 rows, 300 x 300 3.2 | 4.9;  4 rows, 2000 x 2000 8.0 | 6.4
+static bool mx_rows_pay(int N, int K, int M, int log2_most) { return (double)N * K * M <= (double)(1ll << log2_most); }
+
 extern "C" size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype) {
   if (N <= 0 || K <= 0 || M <= 0 || !aiq::mx_dtype_ok(dtype)) return 0;
-  return aiq::mx_tc_workspace_bytes(K, M, dtype);
+  return mx_rows_pay(N, K, M, M <= 4 ? 24 : 22) ? 0 : aiq::mx_tc_workspace_bytes(K, M, dtype);
 }
 
 extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
@@ -420,7 +495,6 @@ extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, con
   if (aiq_status_t st = mx_check_rows("aiq_mx_linear", x, dtype, x_stride)) return st;
   if (aiq_status_t st = mx_check_out("aiq_mx_linear", y, dtype, M, N, y_stride)) return st;
   if (aiq_status_t st = mx_check_bias("aiq_mx_linear", bias)) return st;
-  if (aiq_status_t st = aiq::check_device_sm100()) return st;
   aiq::MxProduct p = {};
   p.w_codes = static_cast<const uint8_t*>(codes);
   p.w_scales = static_cast<const uint8_t*>(scales);
@@ -428,14 +502,13 @@ extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, con
   p.x = x; p.x_stride = x_stride;
   p.y = y; p.y_stride = y_stride;
   p.N = N; p.K = K; p.M = M; p.dtype = dtype;
-  if (workspace) {
-    if (((uintptr_t)workspace) & 15) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear: workspace not 16-byte aligned");
-    if (workspace_bytes < aiq::mx_tc_workspace_bytes(K, M, dtype))
-      return set_error(AIQ_ERR_WORKSPACE_TOO_SMALL, "aiq_mx_linear: workspace of %zu bytes, %zu needed", workspace_bytes,
-                       aiq::mx_tc_workspace_bytes(K, M, dtype));
-    return aiq::launch_mx_product_tc(p, workspace, (cudaStream_t)stream);
-  }
-  return aiq::launch_mx_product_plain(p, (cudaStream_t)stream);
+  if (((uintptr_t)workspace) & 15) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear: workspace not 16-byte aligned");
+  const size_t needed = aiq_mx_linear_workspace_bytes(N, K, M, dtype);
+  if (workspace && workspace_bytes < needed)
+    return set_error(AIQ_ERR_WORKSPACE_TOO_SMALL, "aiq_mx_linear: workspace of %zu bytes, %zu needed", workspace_bytes, needed);
+  if (aiq_status_t st = aiq::check_device_sm100()) return st;
+  if (needed == 0 || !workspace) return aiq::launch_mx_product_rows(p, (cudaStream_t)stream);
+  return aiq::launch_mx_product_tc(p, workspace, (cudaStream_t)stream);
 }
 
 extern "C" aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales, int M, const void* b_codes, const void* b_scales, int N,
@@ -453,5 +526,6 @@ extern "C" aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales,
   p.x_scales = static_cast<const uint8_t*>(a_scales);
   p.y = y; p.y_stride = y_stride;
   p.N = N; p.K = K; p.M = M; p.dtype = dtype;
+  if (mx_rows_pay(N, K, M, M == 1 ? 23 : 22)) return aiq::launch_mx_product_rows(p, (cudaStream_t)stream);
   return aiq::launch_mx_product_tc(p, nullptr, (cudaStream_t)stream);
 }

@@ -34,8 +34,8 @@ aiq_status_t launch_mx_quantize(const void* x, int dtype, int rows, int K, int64
                                 cudaStream_t s);
 aiq_status_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int rows, int K, int dtype, void* y,
                                   int64_t y_stride, cudaStream_t s);
-// any shape, no workspace
-aiq_status_t launch_mx_product_plain(const MxProduct& p, cudaStream_t s);
+// any shape, no workspace: a few rows of x, small matrices
+aiq_status_t launch_mx_product_rows(const MxProduct& p, cudaStream_t s);
 // tensor cores (mx_tc.cu); with x not microscaled: needs the workspace, for x as eight-bit pieces
 size_t mx_tc_workspace_bytes(int K, int M, int dtype);
 aiq_status_t launch_mx_product_tc(const MxProduct& p, void* workspace, cudaStream_t s);

@@ -20,15 +20,17 @@
 //   warp 1     MMA issuer              warp 3   TMA: scale bytes of both, 512 k at a time (16 bytes a row)
 //   warps 4-7  scale bytes: shared memory -> tensor memory, where the MMA reads them: four k blocks of a row in a column's
 //              32-bit word, rows 32 to a column, the same in each quarter of the lanes
-//   warps 8-11 sums: tensor memory -> registers / shared memory
-// A K range may be split over the CTAs of a cluster; their sums meet in shared memory in a fixed order.
+//   warps 8-15 sums: tensor memory -> registers -> y (two warps to a quarter of the lanes, half of the columns each)
+// Many tiles: one CTA per SM takes every gridDim-th; the sums leave tensor memory within microseconds and are written while
+// the next tile's MMAs run.  Few tiles: the K range is split over the CTAs of a cluster, whose sums meet in shared memory in a
+// fixed order.
 #include "mx.cuh"
 #include "tc_ptx.cuh"
 
 namespace aiq {
 namespace {
 
-constexpr int kMxTcThreads = 12 * 32;
+constexpr int kMxTcThreads = 16 * 32;
 constexpr int kMxATile = 128 * 128;          // bytes of 128 rows of weights in shared memory
 constexpr int kMxACopied = 128 * 64;         // bytes that a copy counts which expands four-bit codes: those of the codes
 constexpr int kMxSuper = 512;                // k per set of scale bytes
@@ -43,12 +45,14 @@ struct MxKind {
 
 struct MxTcParams {
   int N, M;
+  int y_vec;                // rows of y start on four values
   int Mt;                   // rows of x per tile
   int pieces;               // KIND 1: eight-bit pieces of x
   int stack;                // 1: the pieces' rows are one operand
   int rows;                 // rows of a B operand: Mt, stacked pieces * Mt
   int n_chunks, supers_per_split;
   int cluster;
+  int m_blocks, tiles;      // tiles: row blocks * m_blocks
   int a_stages, b_stages;
   int b_cols;               // scale columns of a B operand (a multiple of 4)
   int sf_col, sf_group;     // first scale column, columns per 128 k
@@ -56,29 +60,49 @@ struct MxTcParams {
 };
 
 __host__ __device__ inline int mx_b_unit(int rows) { return rows * 128; }
-// rings of codes, then the sums of the tile in their place; [row of x][128 channels]
+// rings of codes; with a split K range, the sums of the tile in their place afterwards, [row of x][128 channels]
 __host__ __device__ inline int mx_ring_bytes(const MxTcParams& p) {
-  const int rings = p.a_stages * kMxATile + p.b_stages * mx_b_unit(p.rows), sums = p.Mt * 128 * 4;
+  const int rings = p.a_stages * kMxATile + p.b_stages * mx_b_unit(p.rows), sums = p.cluster > 1 ? p.Mt * 128 * 4 : 0;
   return rings > sums ? rings : sums;
 }
 __host__ __device__ inline int mx_scale_tile(const MxTcParams& p) { return (128 + p.b_cols * 32 * (p.stack ? 1 : p.pieces)) * 16; }
 inline int mx_smem_bytes(const MxTcParams& p) {
-  return 1024 + mx_ring_bytes(p) + kMxScaleStages * mx_scale_tile(p) + 8 * (2 * p.a_stages + 2 * p.b_stages + 2 * kMxScaleStages + 10) + 16 + 512;
+  return 1024 + mx_ring_bytes(p) + kMxScaleStages * mx_scale_tile(p) + 8 * (2 * p.a_stages + 2 * p.b_stages + 2 * kMxScaleStages + 10) + 16;
 }
 
-// one MMA; the scale columns and their byte in the words are part of the call
+// The four MMAs of 128 bytes of the operands' rows, and the commits that free the operands; one election.  accumulate: the first
+// one adds to what is there, too.  group: scale columns per 128 k.  bar_a: 0 = the weights stay.
 template <int KIND>
-__device__ __forceinline__ void mx_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+__device__ __forceinline__ void mx_mma4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t group,
+                                        uint32_t accumulate, uint32_t bar_b, uint32_t bar_a) {
   if (KIND == 0)
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+        "{\n\t.reg .pred p, q, r;\n\t.reg .b64 x, y;\n\t.reg .b32 i, u, v;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %7, 0;\n\t"
+        "setp.ne.and.b32 r, %9, 0, q;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+        "add.s64 x, %1, 2;\n\tadd.s64 y, %2, 2;\n\tadd.u32 i, %3, 0x40000020;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, i, [%4], [%5], 1;\n\t"
+        "add.s64 x, %1, 4;\n\tadd.s64 y, %2, 4;\n\tadd.u32 u, %4, %6;\n\tadd.u32 v, %5, %6;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, %3, [u], [v], 1;\n\t"
+        "add.s64 x, %1, 6;\n\tadd.s64 y, %2, 6;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], x, y, i, [u], [v], 1;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%8];\n\t"
+        "@r tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%9];\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(group), "r"(accumulate), "r"(bar_b), "r"(bar_a) : "memory");
   else
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+        "{\n\t.reg .pred p, q, r;\n\t.reg .b64 x, y;\n\t.reg .b32 i;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "setp.ne.and.b32 r, %8, 0, q;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+        "add.s64 x, %1, 2;\n\tadd.s64 y, %2, 2;\n\tadd.u32 i, %3, 0x20000010;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], x, y, i, [%4], [%5], 1;\n\t"
+        "add.s64 x, %1, 4;\n\tadd.s64 y, %2, 4;\n\tadd.u32 i, %3, 0x40000020;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], x, y, i, [%4], [%5], 1;\n\t"
+        "add.s64 x, %1, 6;\n\tadd.s64 y, %2, 6;\n\tadd.u32 i, %3, 0x60000030;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], x, y, i, [%4], [%5], 1;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n\t"
+        "@r tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%8];\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(bar_b), "r"(bar_a) : "memory");
 }
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -101,6 +125,22 @@ __device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMa
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 
+// Bounded wait of the issuing warp, in line and decided by votes: a call would have everything that lives across it moved out of
+// the uniform registers, and an MMA whose operands are not in those takes 180 cycles to issue instead of 40.
+__device__ __forceinline__ bool mbar_wait_uniform(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  const long long t0 = clock64();
+  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if ((i & 63u) == 63u) {
+      const bool over = clock64() - t0 > kWaitLimitCycles;
+      if (__any_sync(0xffffffffu, over || *abort_flag != 0)) break;
+    }
+  }
+  *abort_flag = 1;
+  return false;
+}
+
 // A ring of copies as its producer sees it: wait for the slot, remember the copy; drain() before the CTA may end.
 struct RingCursor {
   uint32_t stage = 0, phase = 0, issued = 0, issued_phase = 0;
@@ -118,18 +158,112 @@ struct RingCursor {
   }
 };
 
+template <typename T>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+  if (sizeof(T) == 4) return 0u;
+  T h[2] = {from_float<T>(a), from_float<T>(b)};
+  return *reinterpret_cast<const uint32_t*>(h);
+}
+
+// 16 columns (rows of y) of a warp's 32 channels; dst: this lane's channel n in the first of them.  Where rows of y of a
+// 16-bit type start on 8 bytes, four lanes exchange their values of four rows, so that each then writes four channels of one row.
+template <typename T>
+__device__ __forceinline__ void store_columns(T* dst, int64_t y_stride, const float* f, int vec, int n, int N, int live, int lane) {
+  const int j = lane & 3;
+  if (sizeof(T) == 4) {
+    if (n < N) {
+#pragma unroll
+      for (int c = 0; c < 16; ++c)
+        if (c < live) dst[c * y_stride] = from_float<T>(f[c]);
+    }
+  } else if (vec && n - lane + 32 <= N) {
+#pragma unroll
+    for (int c = 0; c < 16; c += 4) {
+      const uint32_t p01 = pack_pair<T>(f[c], f[c + 1]), p23 = pack_pair<T>(f[c + 2], f[c + 3]);
+      const uint32_t far = __shfl_xor_sync(0xffffffffu, j < 2 ? p23 : p01, 2), own = j < 2 ? p01 : p23;
+      // rows (0, 1) or (2, 3) of channels j and j ^ 2, the lower channel first
+      const uint32_t lo = j < 2 ? own : far, hi = j < 2 ? far : own;
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, __byte_perm(lo, hi, (j & 1) ? 0x5410 : 0x7632), 1);
+      const uint32_t mine = __byte_perm(lo, hi, (j & 1) ? 0x7632 : 0x5410);       // this lane's row: channels (j, j + 2) or their neighbours'
+      const uint32_t even = (j & 1) ? other : mine, odd = (j & 1) ? mine : other;
+      if (c + j < live) *reinterpret_cast<uint2*>(dst - j + (c + j) * y_stride) = make_uint2(__byte_perm(even, odd, 0x5410), __byte_perm(even, odd, 0x7632));
+    }
+  } else if (n < N) {
+#pragma unroll
+    for (int c = 0; c < 16; ++c)
+      if (c < live) dst[c * y_stride] = from_float<T>(f[c]);
+  }
+}
+
+// ---- x as eight-bit pieces --------------------------------------------------------------------------
+template <typename T> struct PieceCount { static constexpr int N = 5; };
+template <> struct PieceCount<__half> { static constexpr int N = 3; };
+template <> struct PieceCount<__nv_bfloat16> { static constexpr int N = 2; };
+
+// eight values of a row from k on (a multiple of 8), zero from K on
+template <typename T>
+__device__ __forceinline__ void load_x(const T* row, int k, int K, int vec, float* f) {
+  if (vec && k + 8 <= K) {
+    load8(row + k, f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = k + j < K ? to_float(row[k + j]) : 0.f;
+  }
+}
+
+// A lane has eight values, four neighbours a block of 32; every lane of the warp takes part.  Piece 0 is the values times the power
+// of two that brings the block's largest into [128, 256), rounded to four bits; what is left, at most 2^-5 of the unit above, times
+// 32, is the next piece's input.  put(piece, eight codes, scale byte).
+template <int PIECES, typename F>
+__device__ __forceinline__ void to_pieces(float* f, F put) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const uint32_t e = top >> 23;
+  const bool dead = e == 255;                      // a NaN or an infinity: scale byte 255 makes the block NaN
+  uint32_t s = dead ? 255u : e < 7 ? 0u : e - 7;
+  float up = mx_inverse_scale(s);
+#pragma unroll
+  for (int q = 0; q < PIECES; ++q) {
+    uint32_t out[2] = {0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = f[2 * j] * up, b = f[2 * j + 1] * up;
+      uint16_t c;
+      uint32_t back;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(b), "f"(a));
+      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(c));
+      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&back));
+      f[2 * j] = a - v.x;
+      f[2 * j + 1] = b - v.y;
+      out[j >> 1] |= (uint32_t)c << ((j & 1) * 16);
+    }
+    put(q, dead ? make_uint2(0u, 0u) : make_uint2(out[0], out[1]), s);
+    if (!dead) {
+      const uint32_t next = s < 5 ? 0u : s - 5;
+      up = (float)(1u << (s - next));
+      s = next;
+    }
+  }
+}
+
 template <int KIND, typename T>
 __global__ void __launch_bounds__(kMxTcThreads, 1)
 mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ CUtensorMap sa_map,
              const __grid_constant__ CUtensorMap sb_map, const __grid_constant__ MxTcParams p, const float* __restrict__ bias,
-             T* __restrict__ y, int64_t y_stride, int vec) {
+             T* __restrict__ y, int64_t y_stride) {
   using Kd = MxKind<KIND>;
-  constexpr bool PROMOTE = sizeof(T) == 4;
+  constexpr bool PROMOTE = sizeof(T) == 4, CHAINED = KIND == 1;       // CHAINED: behind the pre-pass
+  const int vec = p.y_vec;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // Broadcast, so that the compiler sees values that are the same in the whole warp and keeps what the tensor-core instructions take
+  // in uniform registers: with plain tid >> 5 and the address as it lies in shared memory an MMA took 180 to 250 cycles to issue.
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int rank = blockIdx.x % p.cluster;
-  const int n0 = (int)(blockIdx.x / p.cluster) * 128, m0 = blockIdx.y * p.Mt;
+  const int first = blockIdx.x / p.cluster, step = gridDim.x / p.cluster;      // this CTA's tiles
   const int a_stages = p.a_stages, b_stages = p.b_stages, units = p.stack ? 1 : p.pieces;
   const int b_unit = mx_b_unit(p.rows), scale_tile = mx_scale_tile(p);
   const int c_begin = min(p.n_chunks, rank * p.supers_per_split * Kd::CPS);
@@ -148,114 +282,138 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   const uint32_t retired = d_empty + 16;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 2 * a_stages + 2 * b_stages + 2 * kMxScaleStages + 10);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  float* s_bias = reinterpret_cast<float*>(s_tmem + 4);
 
-  if (tid == 0) {
-    for (int i = 0; i < a_stages; ++i) { mbar_init(a_full + 8 * i, 1); mbar_init(a_empty + 8 * i, 1); }
-    for (int i = 0; i < b_stages; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
-    for (int i = 0; i < kMxScaleStages; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_empty + 8 * i, 4); }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(t_full + 8 * i, 4);
-      mbar_init(t_empty + 8 * i, 1);
-      mbar_init(d_full + 8 * i, 1);
-      mbar_init(d_empty + 8 * i, 4);
+  // warp 0: the first copies leave before the other warps are set up, the scale bytes of the weights before the weights themselves
+  RingCursor ar;
+  int a_tile = first, a_chunk = c_begin;
+  auto send_a = [&]() {
+    tma_fill_2d(smem_u32(aring) + ar.stage * kMxATile, &a_map, a_full + 8 * ar.stage, KIND == 0 ? kMxATile : kMxACopied, a_chunk * 128,
+                a_tile / p.m_blocks * 128);
+    ar.sent(a_stages);
+    if (++a_chunk == c_end) { a_chunk = c_begin; a_tile += step; }
+  };
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int i = 0; i < a_stages; ++i) { mbar_init(a_full + 8 * i, 1); mbar_init(a_empty + 8 * i, 1); }
+      for (int i = 0; i < b_stages; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
+      for (int i = 0; i < kMxScaleStages; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_empty + 8 * i, 4); }
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(t_full + 8 * i, 4);
+        mbar_init(t_empty + 8 * i, 1);
+        mbar_init(d_full + 8 * i, 1);
+        mbar_init(d_empty + 8 * i, 8);
+      }
+      mbar_init(retired, 1);
+      *s_abort = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    mbar_init(retired, 1);
-    *s_abort = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (tid >= 256) {
-    const int n = n0 + tid - 256;
-    s_bias[tid - 256] = bias && n < p.N ? bias[n] : 0.f;
-  }
-  __syncthreads();
-  if (warp == 1) {
+    __syncwarp();
+    if (chunks > 0 && first < p.tiles) tma_fill_2d(smem_u32(sring), &sa_map, s_full, (uint32_t)((128 + p.rows * units) * 16), c_begin / Kd::CPS * 16, first / p.m_blocks * 128);
+    if (chunks > 0)
+      for (int i = 0; i < a_stages && a_tile < p.tiles; ++i) send_a();
+  } else if (warp == 1) {
     tmem_alloc(smem_u32(s_tmem), (uint32_t)p.tmem_cols);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_base = *s_tmem;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, *s_tmem, 0);
   bool alive = true;
 
   if (warp == 0) {
-    RingCursor r;
-    for (int c = c_begin; c < c_end; ++c) {
-      alive = mbar_wait_warp(a_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+    while (chunks > 0 && a_tile < p.tiles) {
+      alive = mbar_wait_warp(a_empty + 8 * ar.stage, ar.phase ^ 1u, s_abort, nullptr);
       if (!alive) break;
-      tma_fill_2d(smem_u32(aring) + r.stage * kMxATile, &a_map, a_full + 8 * r.stage, KIND == 0 ? kMxATile : kMxACopied, c * 128, n0);
-      r.sent(a_stages);
+      send_a();
     }
-    r.drain(a_full, a_stages);
+    ar.drain(a_full, a_stages);
   } else if (warp == 2) {
-    if (KIND == 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
     RingCursor r;
-    for (int c0 = c_begin; c0 < c_end && alive; c0 += Kd::CPS)
-      for (int u = units - 1; u >= 0 && alive; --u)
-        for (int c = c0; c < min(c0 + Kd::CPS, c_end); ++c) {
-          alive = mbar_wait_warp(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
-          if (!alive) break;
-          tma_fill_3d(smem_u32(bring) + r.stage * b_unit, &b_map, b_full + 8 * r.stage, (uint32_t)b_unit, c * 128, m0, u);
-          r.sent(b_stages);
-        }
+    for (int tile = first; tile < p.tiles && alive; tile += step) {
+      const int m0 = tile % p.m_blocks * p.Mt;
+      for (int c0 = c_begin; c0 < c_end && alive; c0 += Kd::CPS)
+        for (int u = units - 1; u >= 0 && alive; --u)
+          for (int c = c0; c < min(c0 + Kd::CPS, c_end); ++c) {
+            alive = mbar_wait_warp(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+            if (!alive) break;
+            tma_fill_3d(smem_u32(bring) + r.stage * b_unit, &b_map, b_full + 8 * r.stage, (uint32_t)b_unit, c * 128, m0, u);
+            r.sent(b_stages);
+          }
+    }
     r.drain(b_full, b_stages);
   } else if (warp == 3) {
-    if (KIND == 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
     RingCursor r;
-    for (int s = 0; s < supers; ++s) {
-      alive = mbar_wait_warp(s_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
-      if (!alive) break;
-      const uint32_t dst = smem_u32(sring) + r.stage * scale_tile, bar = s_full + 8 * r.stage;
-      const int byte = (c_begin / Kd::CPS + s) * 16;
-      expect_tx_elect(bar, (uint32_t)((128 + p.rows * units) * 16));
-      tma_load_2d_elect(dst, &sa_map, bar, byte, n0);
-      for (int u = 0; u < units; ++u) tma_load_3d_elect(dst + (128 + u * p.b_cols * 32) * 16, &sb_map, bar, byte, m0, u);
-      r.sent(kMxScaleStages);
+    for (int tile = first; tile < p.tiles && alive; tile += step) {
+      const int n0 = tile / p.m_blocks * 128, m0 = tile % p.m_blocks * p.Mt;
+      for (int s = 0; s < supers; ++s) {
+        alive = mbar_wait_warp(s_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+        if (!alive) break;
+        const uint32_t dst = smem_u32(sring) + r.stage * scale_tile, bar = s_full + 8 * r.stage;
+        const int byte = (c_begin / Kd::CPS + s) * 16;
+        if (tile != first || s != 0) {              // the very first by warp 0
+          expect_tx_elect(bar, (uint32_t)((128 + p.rows * units) * 16));
+          tma_load_2d_elect(dst, &sa_map, bar, byte, n0);
+        }
+        for (int u = 0; u < units; ++u) tma_load_3d_elect(dst + (128 + u * p.b_cols * 32) * 16, &sb_map, bar, byte, m0, u);
+        r.sent(kMxScaleStages);
+      }
     }
     r.drain(s_full, kMxScaleStages);
   } else if (warp == 1) {
     // ---- MMA issuer: all 32 lanes converged, one elected lane issues --------------------------------
+    // The answer of a look at a barrier takes about a hundred cycles, as long as several narrow MMAs: whether the next step's
+    // operands are there is asked before this step's MMAs are issued.
     constexpr uint32_t DESC_HI = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);   // SBO 1024, version 1, 128-byte swizzle
     constexpr uint32_t LBO_FIELD = 1u << 16;
     // operand types, N, scales in powers of two, M = 128
     const uint32_t idesc = (KIND == 0 ? (1u << 7) | (1u << 10) : (5u << 7)) | ((uint32_t)(p.rows >> 3) << 17) | (1u << 23) | (1u << 27);
     // The smallest pieces come first: while they are added up the sums are small, and so is what the additions drop.
-    uint32_t as = 0, aph = 0, bs = 0, bph = 0;
-    for (int s = 0; s < supers && alive; ++s) {
-      const uint32_t tb = s & 1, tph = (s >> 1) & 1;
-      uint32_t accumulate = !PROMOTE && s > 0;
-      if (PROMOTE) alive = mbar_wait_warp(d_empty + 8 * tb, tph ^ 1u, s_abort, nullptr);
-      alive = alive && mbar_wait_warp(t_full + 8 * tb, tph, s_abort, nullptr);
-      const uint32_t d = tmem_base + (PROMOTE ? tb * p.rows : 0);
-      const uint32_t sf = tmem_base + p.sf_col + tb * 4 * p.sf_group;
-      const int n = min(Kd::CPS, chunks - s * Kd::CPS);
-      for (int u = units - 1; u >= 0 && alive; --u) {
-        uint32_t at = as, atph = aph;
-        for (int cc = 0; cc < n; ++cc) {
-          alive = (u != units - 1 || mbar_wait_warp(a_full + 8 * at, atph, s_abort, nullptr)) &&
-                  mbar_wait_warp(b_full + 8 * bs, bph, s_abort, nullptr);
-          if (!alive) break;
-          tc_fence_after();
-          const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(aring) + at * kMxATile) >> 4) | LBO_FIELD);
-          const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(bring) + bs * b_unit) >> 4) | LBO_FIELD);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t group = KIND == 0 ? 2 * cc + (i >> 1) : cc, id = KIND == 0 ? (i & 1) * 2 : i;
-            const uint32_t sfa = sf + group * p.sf_group;
-            mx_mma<KIND>(d, adesc + 2 * i, bdesc + 2 * i, idesc | (id << 4) | (id << 29), sfa, sfa + 4 + u * p.b_cols, accumulate);
+    uint32_t as = 0, aph = 0, bs = 0, bph = 0, sets = 0, done = 0;               // sets, done: of all tiles so far
+    bool ready = false, t_ready = false;
+    for (int tile = first; tile < p.tiles && alive; tile += step, ++done) {
+      if (!PROMOTE && supers > 0) alive = mbar_wait_uniform(d_empty, (done & 1) ^ 1u, s_abort);
+      for (int s = 0; s < supers && alive; ++s, ++sets) {
+        const uint32_t tb = sets & 1, tph = (sets >> 1) & 1;
+        uint32_t accumulate = !PROMOTE && s > 0;
+        if (PROMOTE) alive = mbar_wait_uniform(d_empty + 8 * tb, tph ^ 1u, s_abort);
+        if (!t_ready) alive = alive && mbar_wait_uniform(t_full + 8 * tb, tph, s_abort);
+        if (!alive) break;
+        t_ready = false;
+        const uint32_t d = tmem_base + (PROMOTE ? tb * p.rows : 0);
+        const uint32_t sf = tmem_base + p.sf_col + tb * 4 * p.sf_group;
+        const int n = min(Kd::CPS, chunks - s * Kd::CPS);
+        for (int u = units - 1; u >= 0 && alive; --u) {
+          uint32_t at = as, atph = aph;
+          for (int cc = 0; cc < n; ++cc) {
+            if (!ready) {
+              alive = mbar_wait_uniform(a_full + 8 * at, atph, s_abort) && mbar_wait_uniform(b_full + 8 * bs, bph, s_abort);
+              if (!alive) break;
+            }
+            tc_fence_after();
+            const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(aring) + at * kMxATile) >> 4) | LBO_FIELD);
+            const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(bring) + bs * b_unit) >> 4) | LBO_FIELD);
+            const uint32_t sfa = sf + (KIND == 0 ? 2 * cc : cc) * p.sf_group, sfb = sfa + 4 + u * p.b_cols;
+            const uint32_t b_done = b_empty + 8 * bs, a_done = u == 0 ? a_empty + 8 * at : 0u;
+            if (++bs == (uint32_t)b_stages) { bs = 0; bph ^= 1u; }
+            if (++at == (uint32_t)a_stages) { at = 0; atph ^= 1u; }
+            const bool last = cc + 1 == n;
+            if (last && u == 0) { as = at; aph = atph; }
+            const uint32_t na = last ? as : at, naph = last ? aph : atph;
+            const bool next_ready = mbar_test(a_full + 8 * na, naph) & mbar_test(b_full + 8 * bs, bph);
+            const bool next_t = last && u == 0 ? mbar_test(t_full + 8 * (tb ^ 1u), ((sets + 1) >> 1) & 1) : false;
+            mx_mma4<KIND>(d, adesc, bdesc, idesc, sfa, sfb, p.sf_group, accumulate, b_done, a_done);
             accumulate = 1;
+            ready = __all_sync(0xffffffffu, next_ready);
+            t_ready = __all_sync(0xffffffffu, next_t);
           }
-          umma_commit(b_empty + 8 * bs);
-          if (++bs == (uint32_t)b_stages) { bs = 0; bph ^= 1u; }
-          if (u == 0) umma_commit(a_empty + 8 * at);
-          if (++at == (uint32_t)a_stages) { at = 0; atph ^= 1u; }
         }
-        if (u == 0) { as = at; aph = atph; }
+        if (!alive) break;
+        umma_commit(t_empty + 8 * tb);
+        if (PROMOTE || s + 1 == supers) umma_commit(d_full + 8 * (PROMOTE ? tb : 0));
       }
-      if (!alive) break;
-      umma_commit(t_empty + 8 * tb);
-      if (PROMOTE || s + 1 == supers) umma_commit(d_full + 8 * (PROMOTE ? tb : 0));
     }
     if (!alive) {                                  // what was issued must end before the CTA does
       umma_commit(retired);
@@ -266,8 +424,9 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     // ---- scale bytes -> tensor memory ----------------------------------------------------------------
     const uint32_t quarter = (uint32_t)(warp & 3) * 32;
     const int cols = p.b_cols * units;
+    const int sets = first < p.tiles ? ((p.tiles - 1 - first) / step + 1) * supers : 0;
     uint32_t stage = 0, phase = 0;
-    for (int s = 0; s < supers; ++s) {
+    for (int s = 0; s < sets; ++s) {
       const uint32_t tb = s & 1, tph = (s >> 1) & 1;
       alive = mbar_wait_warp(s_full + 8 * stage, phase, s_abort, nullptr) && mbar_wait_warp(t_empty + 8 * tb, tph ^ 1u, s_abort, nullptr);
       if (!alive) break;
@@ -292,83 +451,114 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       if (++stage == kMxScaleStages) { stage = 0; phase ^= 1u; }
     }
   } else {
-    // ---- sums -----------------------------------------------------------------------------------------
-    const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-    const int copies = p.stack ? p.pieces : 1;                 // columns that belong to one row of x
-    float* sums = reinterpret_cast<float*>(smem) + (warp & 3) * 32 + lane;
-    if (PROMOTE) {
-      float acc[128];
+    // ---- sums: lane = output channel, column = row of x --------------------------------------------------
+    if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int ch = (warp & 3) * 32 + lane, split = (p.Mt / 16 + 1) / 2 * 16;       // columns of the lower four warps
+    const int c_first = (warp >> 2) == 2 ? 0 : split, half = (warp >> 2) == 2 ? split : p.Mt - split;
+    const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + c_first;
+    const int copies = p.stack ? p.pieces : 1;                 // columns that belong to one row of x, Mt apart
+    float* sums = reinterpret_cast<float*>(smem) + c_first * 128 + ch;
+    uint32_t sets = 0, done = 0;
+    for (int tile = first; tile < p.tiles && alive; tile += step, ++done) {
+      const int n = tile / p.m_blocks * 128 + ch, m0 = tile % p.m_blocks * p.Mt + c_first;
+      const bool direct = p.cluster == 1;
+      const float b = direct && bias && n < p.N ? bias[n] : 0.f;
+      const int live = n < p.N ? min(half, p.M - m0) : 0;      // this lane's columns that are rows of x
+      T* dst = y + (int64_t)m0 * y_stride + n;
+      if (PROMOTE) {
+        float acc[64];
 #pragma unroll
-      for (int i = 0; i < 128; ++i) acc[i] = 0.f;
-      for (int s = 0; s < supers; ++s) {
-        const uint32_t dbuf = s & 1, dph = (s >> 1) & 1;
-        alive = mbar_wait_warp(d_full + 8 * dbuf, dph, s_abort, nullptr);
+        for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+        for (int s = 0; s < supers; ++s, ++sets) {
+          const uint32_t tb = sets & 1, tph = (sets >> 1) & 1;
+          alive = mbar_wait_warp(d_full + 8 * tb, tph, s_abort, nullptr);
+          if (!alive) break;
+          tc_fence_after();
+          for (int q = copies - 1; q >= 0; --q) {              // the smallest pieces first
+            const uint32_t from = taddr + tb * p.rows + q * p.Mt;
+#pragma unroll
+            for (int c0 = 0; c0 < 64; c0 += 8) {
+              if (c0 >= half) break;
+              uint32_t v[8];
+              tmem_ld8(from + c0, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 8; ++j) acc[c0 + j] += __uint_as_float(v[j]);
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(d_empty + 8 * tb);
+        }
+#pragma unroll
+        for (int c = 0; c < 64; ++c) {
+          if (c >= half) break;
+          if (!direct) sums[c * 128] = acc[c];
+          else if (c < live && alive) dst[c * y_stride] = from_float<T>(acc[c] + b);
+        }
+      } else {
+        // Not unrolled: code that a block runs once per tile comes from far away (unrolled, 16 columns took 1,000 cycles).
+        if (supers > 0) alive = mbar_wait_warp(d_full, done & 1, s_abort, nullptr);
         if (!alive) break;
         tc_fence_after();
-        for (int q = copies - 1; q >= 0; --q) {                // the smallest pieces first
-          const uint32_t from = taddr + dbuf * p.rows + q * p.Mt;
+        T* out = dst;
+#pragma unroll 1
+        for (int c0 = 0; c0 < half; c0 += 16) {
+          float f[16];
 #pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 16) {
-            if (c0 >= p.Mt) break;
-            uint32_t v[16];
-            tmem_ld16(from + c0, v);
-            tmem_ld_wait();
+          for (int j = 0; j < 16; ++j) f[j] = b;
+          if (supers > 0) {
+#pragma unroll 1
+            for (int q = copies - 1; q >= 0; --q) {
+              uint32_t v[16];
+              tmem_ld16(taddr + q * p.Mt + c0, v);
+              tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[c0 + j] += __uint_as_float(v[j]);
+              for (int j = 0; j < 16; ++j) f[j] += __uint_as_float(v[j]);
+            }
+          }
+          if (!direct) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sums[(c0 + j) * 128] = f[j];
+          } else {
+            store_columns<T>(out, y_stride, f, vec, n, p.N, p.M - m0 - c0, lane);
+            out += 16 * y_stride;
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(d_empty + 8 * dbuf);
-      }
-      // the rings are free once the last sums are complete: every copy has landed and been read
-#pragma unroll
-      for (int c0 = 0; c0 < 128; c0 += 16) {
-        if (c0 >= p.Mt) break;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) sums[(c0 + j) * 128] = acc[c0 + j];
-      }
-    } else {
-      if (supers > 0) alive = mbar_wait_warp(d_full, 0, s_abort, nullptr);
-      tc_fence_after();
-      for (int c0 = 0; c0 < p.Mt; c0 += 8) {
-        float f[8] = {};
-        if (supers > 0 && alive) {
-          for (int q = copies - 1; q >= 0; --q) {
-            uint32_t v[8];
-            tmem_ld8(taddr + q * p.Mt + c0, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(v[j]);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sums[(c0 + j) * 128] = f[j];
+        if (lane == 0) mbar_arrive(d_empty);
       }
     }
   }
 
-  // ---- sums of the cluster -> y, a row of 128 channels per warp -------------------------------------
   tc_fence_before();
   __syncthreads();
-  if (*s_abort) {                                  // a wait that ran out shows in the result
-    for (int i = tid; i < p.Mt * 128; i += kMxTcThreads) reinterpret_cast<float*>(smem)[i] = __int_as_float(0x7FC00000);
-    __syncthreads();
-  }
-  if (p.cluster > 1) {
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-  }
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
   }
-  if (KIND == 1) asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int rows = min(p.Mt, p.M - m0);
+  if (p.cluster == 1) {
+    if (*s_abort) {                                // a wait that ran out shows in the result
+      for (int tile = first; tile < p.tiles; tile += step) {
+        const int n0 = tile / p.m_blocks * 128, m0 = tile % p.m_blocks * p.Mt;
+        for (int i = tid; i < p.Mt * 128; i += kMxTcThreads)
+          if (m0 + i / 128 < p.M && n0 + i % 128 < p.N) y[(int64_t)(m0 + i / 128) * y_stride + n0 + i % 128] = from_float<T>(__int_as_float(0x7FC00000));
+      }
+    }
+    return;
+  }
+
+  // ---- sums of the cluster -> y, a row of 128 channels per warp -------------------------------------
+  if (*s_abort)
+    for (int i = tid; i < p.Mt * 128; i += kMxTcThreads) reinterpret_cast<float*>(smem)[i] = __int_as_float(0x7FC00000);
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int n0 = first / p.m_blocks * 128, m0 = first % p.m_blocks * p.Mt, rows = min(p.Mt, p.M - m0);
   for (int r = rank + warp * p.cluster; r < rows; r += (kMxTcThreads / 32) * p.cluster) {
     T* dst = y + (int64_t)(m0 + r) * y_stride + n0;
-    if (vec) {                                                 // rows of y start on four values: a lane takes four channels
-      float4 v = *reinterpret_cast<const float4*>(s_bias + lane * 4);
+    if (vec && n0 + lane * 4 + 4 <= p.N) {                     // rows of y start on four values: a lane takes four channels
       const uint32_t mine = smem_u32(smem) + (uint32_t)(r * 128 + lane * 4) * 4;
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int q = 0; q < p.cluster; ++q) {
@@ -379,24 +569,21 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
                      : "=f"(part.x), "=f"(part.y), "=f"(part.z), "=f"(part.w) : "r"(theirs) : "memory");
         sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
       }
-      v.x += sum.x; v.y += sum.y; v.z += sum.z; v.w += sum.w;
-      if (n0 + lane * 4 + 4 <= p.N) {
-        if (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(dst + lane * 4) = v;
-        } else {
-          T h[4] = {from_float<T>(v.x), from_float<T>(v.y), from_float<T>(v.z), from_float<T>(v.w)};
-          *reinterpret_cast<uint2*>(dst + lane * 4) = *reinterpret_cast<const uint2*>(h);
-        }
-        continue;
+      if (bias) {
+        const float* b = bias + n0 + lane * 4;
+        sum.x += b[0]; sum.y += b[1]; sum.z += b[2]; sum.w += b[3];
       }
-      const float f[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (n0 + lane * 4 + j < p.N) dst[lane * 4 + j] = from_float<T>(f[j]);
+      if (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(dst + lane * 4) = sum;
+      } else {
+        T h[4] = {from_float<T>(sum.x), from_float<T>(sum.y), from_float<T>(sum.z), from_float<T>(sum.w)};
+        *reinterpret_cast<uint2*>(dst + lane * 4) = *reinterpret_cast<const uint2*>(h);
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int ch = lane + 32 * j;
+        const int ch = vec ? lane * 4 + j : lane + 32 * j;
+        if (n0 + ch >= p.N) continue;
         const uint32_t mine = smem_u32(smem) + (uint32_t)(r * 128 + ch) * 4;
         float sum = 0.f;
         for (int q = 0; q < p.cluster; ++q) {
@@ -406,24 +593,20 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
           asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(theirs) : "memory");
           sum += part;
         }
-        if (n0 + ch < p.N) dst[ch] = from_float<T>(sum + s_bias[ch]);
+        dst[ch] = from_float<T>(sum + (bias ? bias[n0 + ch] : 0.f));
       }
     }
   }
-  if (p.cluster > 1) {                                         // no CTA leaves while another reads its sums
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-  }
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");      // no CTA leaves while another reads its sums
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // ---------------------------------------------------------------------------------------
-// x -> eight-bit pieces
+// x -> eight-bit pieces, for a large batch
 // ---------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 256;
 
-// A lane takes eight values, four lanes a block.  Piece 0 is the values times the power of two that brings the block's largest
-// into [128, 256), rounded to four bits; what is left, at most 2^-5 of the unit above, times 32, is the next piece's input.
-template <typename T, int PIECES>
+template <typename T>
 __global__ void __launch_bounds__(kSplitThreads)
 mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int M, int vec, FastDiv words, int scale_row, uint64_t units,
                   uint2* __restrict__ planes, uint8_t* __restrict__ scales) {
@@ -432,64 +615,33 @@ mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int M, int v
   const bool live = u < units;
   const uint32_t row = live ? (uint32_t)(u < (1ull << 31) ? words.div((uint32_t)u) : u / words.d) : 0u;
   const uint32_t word = live ? (uint32_t)(u - (uint64_t)row * words.d) : 0u;
-  const int k = (int)word * 8;
-  const T* src = x + (int64_t)row * x_stride + k;
   float f[8];
-  if (vec && live && k + 8 <= K) {
-    load8(src, f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = live && k + j < K ? to_float(src[j]) : 0.f;
-  }
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  if (!live) return;
-  const uint32_t e = top >> 23;
-  const bool dead = e == 255;
-  uint32_t s = dead ? 255u : e < 7 ? 0u : e - 7;
-  float up = mx_inverse_scale(s);
+  load_x(x + (int64_t)row * x_stride, (int)word * 8, live ? K : 0, vec, f);
   uint8_t* sr = scales + (int64_t)row * scale_row;
   const int64_t piece_words = (int64_t)M * words.d, piece_scales = (int64_t)M * scale_row;
-#pragma unroll
-  for (int q = 0; q < PIECES; ++q) {
-    uint32_t out[2] = {0u, 0u};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float a = f[2 * j] * up, b = f[2 * j + 1] * up;
-      uint16_t c;
-      uint32_t back;
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(b), "f"(a));
-      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(c));
-      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&back));
-      f[2 * j] = a - v.x;
-      f[2 * j + 1] = b - v.y;
-      out[j >> 1] |= (uint32_t)c << ((j & 1) * 16);
-    }
-    planes[q * piece_words + u] = dead ? make_uint2(0u, 0u) : make_uint2(out[0], out[1]);
+  to_pieces<PieceCount<T>::N>(f, [&](int q, uint2 codes, uint32_t s) {
+    if (!live) return;
+    planes[q * piece_words + u] = codes;
     if ((word & 3) == 0) sr[q * piece_scales + (word >> 2)] = (uint8_t)s;
     if (word + 1 == words.d)
       for (int b = (int)words.d / 4; b < scale_row; ++b) sr[q * piece_scales + b] = 0;
-    if (!dead) {
-      const uint32_t next = s < 5 ? 0u : s - 5;
-      up = (float)(1u << (s - next));
-      s = next;
-    }
-  }
+  });
 }
 
 inline int mx_pieces(int dtype) { return dtype == AIQ_DTYPE_F32 ? 5 : dtype == AIQ_DTYPE_F16 ? 3 : 2; }
 inline int64_t mx_plane_row(int K) { return ((int64_t)K + 127) / 128 * 128; }
 
-template <typename T, int PIECES>
+template <typename T>
+int x_vec(const MxProduct& p) {
+  return p.x && (((uintptr_t)p.x) & 15) == 0 && (p.M == 1 || p.x_stride * (int64_t)sizeof(T) % 16 == 0);
+}
+
+template <typename T>
 aiq_status_t split_x(const MxProduct& p, uint8_t* planes, uint8_t* scales, cudaStream_t s) {
   const uint32_t words = (uint32_t)(mx_plane_row(p.K) / 8);
   const uint64_t units = (uint64_t)p.M * words;
-  const int vec = (((uintptr_t)p.x) & 15) == 0 && (p.M == 1 || p.x_stride * (int64_t)sizeof(T) % 16 == 0);
-  mx_split_x_kernel<T, PIECES><<<(unsigned)((units + kSplitThreads - 1) / kSplitThreads), kSplitThreads, 0, s>>>(
-      static_cast<const T*>(p.x), p.x_stride, p.K, p.M, vec, FastDiv(words), (int)mx_scale_row_bytes(p.K), units,
+  mx_split_x_kernel<T><<<(unsigned)((units + kSplitThreads - 1) / kSplitThreads), kSplitThreads, 0, s>>>(
+      static_cast<const T*>(p.x), p.x_stride, p.K, p.M, x_vec<T>(p), FastDiv(words), (int)mx_scale_row_bytes(p.K), units,
       reinterpret_cast<uint2*>(planes), scales);
   AIQ_LAUNCH_CHECK("mx_split_x");
   return AIQ_OK;
@@ -515,11 +667,12 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
 
   MxTcParams p = {};
   p.N = g.N; p.M = g.M;
-  p.pieces = KIND == 1 ? mx_pieces(g.dtype) : 1;
+  p.pieces = KIND == 1 ? PieceCount<T>::N : 1;
   p.n_chunks = (g.K + Kd::CHUNK - 1) / Kd::CHUNK;
   const int n_super = (g.K + kMxSuper - 1) / kMxSuper, row_blocks = (g.N + 127) / 128;
   // rows of x per tile: the sums of a tile and the scale words have to fit into 512 columns
-  const int widest = PROMOTE ? 128 : 256, stacked = p.pieces == 1 ? widest : (PROMOTE ? 160 : 256) / p.pieces / 16 * 16;
+  const int widest = PROMOTE ? 128 : 256;
+  const int stacked = p.pieces == 1 ? widest : (PROMOTE ? 160 : 256) / p.pieces / 16 * 16;
   p.stack = g.M <= stacked;
   const int most = p.stack ? stacked : widest;
   p.Mt = g.M >= most ? most : (g.M + 15) / 16 * 16;
@@ -530,8 +683,10 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   p.tmem_cols = 32;
   while (p.tmem_cols < p.sf_col + 8 * p.sf_group) p.tmem_cols <<= 1;
   if (p.tmem_cols > 512) return set_error(AIQ_ERR_SHAPE, "mx_tc: %d columns of tensor memory", p.tmem_cols);
-  const int m_blocks = (g.M + p.Mt - 1) / p.Mt;
-  int splits = props.n_sms / (row_blocks * m_blocks);
+  p.m_blocks = (g.M + p.Mt - 1) / p.Mt;
+  if ((int64_t)row_blocks * p.m_blocks > 0x7FFFFFFF) return set_error(AIQ_ERR_SHAPE, "mx_tc: too many tiles");
+  p.tiles = row_blocks * p.m_blocks;
+  const int splits = props.n_sms / p.tiles;
   p.cluster = 1;
   while (p.cluster * 2 <= splits && p.cluster * 2 <= n_super && p.cluster < 8) p.cluster *= 2;
   p.supers_per_split = (n_super + p.cluster - 1) / p.cluster;
@@ -563,6 +718,7 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   {
     const cuuint64_t x_row = KIND == 0 ? w_row : (cuuint64_t)mx_plane_row(g.K), P = p.pieces;
     const uint8_t* codes = KIND == 0 ? g.x_codes : workspace;
+
     const uint8_t* scales = KIND == 0 ? g.x_scales : workspace + P * M * x_row;
     const cuuint64_t dims[3] = {x_row, M, P}, strides[2] = {x_row, x_row * M};
     const cuuint32_t box[3] = {128, (cuuint32_t)p.Mt, (cuuint32_t)(p.stack ? P : 1)};
@@ -573,19 +729,13 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
       return st;
   }
   const int y_step = 4 * (int)sizeof(T);                       // bytes a lane writes
-  const int vec = (((uintptr_t)g.y) % y_step) == 0 && (g.M == 1 || g.y_stride * (int64_t)sizeof(T) % y_step == 0);
+  p.y_vec = (((uintptr_t)g.y) % y_step) == 0 && (g.M == 1 || g.y_stride * (int64_t)sizeof(T) % y_step == 0);
   LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * g.M * g.N * g.K,
                     (double)(g.N + (KIND == 0 ? g.M : 0)) * (w_row + s_row) + sizeof(T) * (double)g.M * (g.N + (KIND == 1 ? g.K : 0)));
-  if (KIND == 1) {
-    uint8_t* scales = workspace + (size_t)p.pieces * M * mx_plane_row(g.K);
-    aiq_status_t st = AIQ_OK;
-    if (sizeof(T) == 4) st = split_x<T, 5>(g, workspace, scales, s);
-    else if (g.dtype == AIQ_DTYPE_F16) st = split_x<T, 3>(g, workspace, scales, s);
-    else st = split_x<T, 2>(g, workspace, scales, s);
-    if (st != AIQ_OK) return st;
-  }
-  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T>, dim3(row_blocks * p.cluster, m_blocks), dim3(kMxTcThreads),
-                                      (size_t)mx_smem_bytes(p), s, a_map, b_map, sa_map, sb_map, p, g.bias, static_cast<T*>(g.y), g.y_stride, vec));
+  if (KIND == 1)
+    if (aiq_status_t st = split_x<T>(g, workspace, workspace + (size_t)p.pieces * M * mx_plane_row(g.K), s)) return st;
+  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T>, dim3(p.cluster > 1 || p.tiles < props.n_sms ? p.tiles * p.cluster : props.n_sms), dim3(kMxTcThreads),
+                                      (size_t)mx_smem_bytes(p), s, a_map, b_map, sa_map, sb_map, p, g.bias, static_cast<T*>(g.y), g.y_stride));
   AIQ_LAUNCH_CHECK("mx_tc");
   return AIQ_OK;
 }
@@ -598,17 +748,10 @@ size_t mx_tc_workspace_bytes(int K, int M, int dtype) {
 
 aiq_status_t launch_mx_product_tc(const MxProduct& p, void* workspace, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  if (p.x) {
-    switch (p.dtype) {
-      case AIQ_DTYPE_F32: return launch_kind<1, float>(p, ws, s);
-      case AIQ_DTYPE_F16: return launch_kind<1, __half>(p, ws, s);
-      default: return launch_kind<1, __nv_bfloat16>(p, ws, s);
-    }
-  }
   switch (p.dtype) {
-    case AIQ_DTYPE_F32: return launch_kind<0, float>(p, ws, s);
-    case AIQ_DTYPE_F16: return launch_kind<0, __half>(p, ws, s);
-    default: return launch_kind<0, __nv_bfloat16>(p, ws, s);
+    case AIQ_DTYPE_F32: return p.x ? launch_kind<1, float>(p, ws, s) : launch_kind<0, float>(p, ws, s);
+    case AIQ_DTYPE_F16: return p.x ? launch_kind<1, __half>(p, ws, s) : launch_kind<0, __half>(p, ws, s);
+    default: return p.x ? launch_kind<1, __nv_bfloat16>(p, ws, s) : launch_kind<0, __nv_bfloat16>(p, ws, s);
   }
 }
 

@@ -77,7 +77,9 @@ def test_every_code_and_scale():
 
 
 SHAPES = [(1, 1, 1), (3, 33, 2), (8, 32, 1), (10, 64, 1), (129, 100, 5), (64, 320, 9), (200, 609, 17), (128, 512, 33), (1280, 320, 1),
-          (1000, 1281, 4), (257, 2500, 130), (512, 1024, 300), (384, 4097, 64), (130, 8192, 3)]
+          (1000, 1281, 4), (257, 2500, 130), (512, 1024, 300), (384, 4097, 64), (130, 8192, 3),
+          # long K ranges per block, more tiles than SMs
+          (9500, 2176, 5), (9500, 2176, 16), (19000, 1100, 7), (1290, 650, 3500)]
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
@@ -186,3 +188,60 @@ def test_quantize_activations_then_multiply():
     check(y, xv.double().cpu().numpy(), wv.double().cpu().numpy(), None, torch.float32, "mx")
     z = linear(wc, ws, None, xv.float(), torch.empty((m, n), device="cuda"))
     check(z, xv.double().cpu().numpy(), wv.double().cpu().numpy(), None, torch.float32, "f32")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_captured_calls_on_two_streams(dtype):
+    """Two graphs on two streams, each with its own workspace, replayed with new inputs in place; bit-equal to eager calls."""
+    b, dt, n, k, m = binding(), TYPES[dtype], 1100, 1500, 70
+    codes, scales = held(weights(n, k, 41))
+    size = b.aiq_mx_linear_workspace_bytes(n, k, m, dt)
+    assert size > 0
+    runs = []
+    for i in range(2):
+        x = activations(m, k, dt, 42 + i)
+        s = torch.cuda.Stream()
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        xc, xs = held(x)
+        y, z = torch.empty((m, n), dtype=dt, device="cuda"), torch.empty((m, n), dtype=dt, device="cuda")
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            b.aiq_mx_quantize(x, xc, xs)
+            b.aiq_mx_matmul(xc, xs, codes, scales, None, k, z)
+            b.aiq_mx_linear(codes, scales, None, x, y, workspace=ws)
+        runs.append((g, s, x, ws, xc, xs, y, z))
+    for rep in range(3):
+        new = [activations(m, k, dt, 50 + 2 * rep + i) for i in range(2)]
+        for (g, s, x, *_), v in zip(runs, new):
+            x.copy_(v)
+        torch.cuda.synchronize()
+        for g, s, *_ in runs:
+            with torch.cuda.stream(s):
+                g.replay()
+                g.replay()
+        torch.cuda.synchronize()
+        for (g, s, x, ws, xc, xs, y, z), v in zip(runs, new):
+            ey = linear(codes, scales, None, v, torch.empty_like(y))
+            vc, vs = held(v)
+            ez = torch.empty_like(z)
+            b.aiq_mx_matmul(vc, vs, codes, scales, None, k, ez)
+            assert torch.equal(y, ey) and torch.equal(z, ez)
+
+
+def test_refusals_on_the_device():
+    b = binding()
+    codes, scales = held(weights(256, 2000, 1))
+    x, y = activations(64, 2000, torch.bfloat16, 2), torch.empty((64, 256), dtype=torch.bfloat16, device="cuda")
+    bad = [dict(x=x.float()), dict(x=x[:, :1800]), dict(x=x.t()), dict(x=x[:32]), dict(y=y[:, :255]), dict(y=y.t()), dict(y=y.expand(1, 64, 256)),
+           dict(x=x.cpu()), dict(codes=codes[:255]), dict(codes=codes[:, :512]), dict(scales=scales.cpu()), dict(x=x.double()),
+           dict(bias=torch.zeros(255, device="cuda")), dict(bias=torch.zeros(256, dtype=torch.float16, device="cuda"))]
+    for change in bad:
+        a = dict(codes=codes, scales=scales, bias=None, x=x, y=y) | change
+        with pytest.raises(ValueError):
+            b.aiq_mx_linear(a["codes"], a["scales"], a["bias"], a["x"], a["y"])
+    with pytest.raises(b.AiqError) as e:
+        b.aiq_mx_linear(codes, scales, None, x, y, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == b.ERR_WORKSPACE_TOO_SMALL
+    with pytest.raises(b.AiqError):                          # rows of y on top of each other
+        b.aiq_mx_linear(codes, scales, None, x, y[:1].expand(64, 256))

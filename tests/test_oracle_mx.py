@@ -70,6 +70,9 @@ def test_refusals_of_the_c_abi(aiq):
     for bad in (dict(c=None), dict(s=None), dict(x=None), dict(y=None), dict(n=0), dict(k=0), dict(m=0), dict(dt=9), dict(ys=7),
                 dict(xs=-2), dict(c=odd16), dict(s=odd), dict(y=odd), dict(b=odd)):
         assert lin(**bad) == E, bad
+    big = dict(n=4096, k=4096, m=64, xs=4096, ys=4096)
+    assert lin(**big, ws=odd, wb=1 << 30) == E and "workspace" in aiq.last_error()
+    assert lin(**big, ws=one, wb=16) == aiq.ERR_WORKSPACE_TOO_SMALL
     mat = lambda ac=one, as_=one, m=4, bc=one, bs=one, n=8, b=None, k=32, y=one, dt=f16, ys=8: \
         L.aiq_mx_matmul(ac, as_, m, bc, bs, n, b, k, y, dt, ys, None)
     for bad in (dict(ac=None), dict(as_=None), dict(bc=None), dict(bs=None), dict(y=None), dict(m=0), dict(n=0), dict(k=0), dict(dt=4),
