@@ -52,12 +52,25 @@ struct MxTcParams {
   int rows;                 // rows of a B operand: Mt, stacked pieces * Mt
   int n_chunks, supers_per_split;
   int cluster;
-  int m_blocks, tiles;      // tiles: row blocks * m_blocks
+  int m_blocks, tiles;      // tiles: row blocks * m_blocks, then the halves of some of them:
+  int full;                 // tiles from this one on are halves of tiles (Mt / 2 rows of x), two for each
+  int box;                  // rows of x per copy: Mt, or Mt / 2 where there are halves
+  int d_bufs;               // sets of sums in tensor memory, used in turn: 2 for float32 results and where they fit
   int a_stages, b_stages;
   int b_cols;               // scale columns of a B operand (a multiple of 4)
   int sf_col, sf_group;     // first scale column, columns per 128 k
   int tmem_cols;
 };
+
+// tile `t` of a launch
+struct MxTile {
+  int n0, m0, Mt;
+};
+__device__ __forceinline__ MxTile mx_tile(const MxTcParams& p, int t) {
+  const bool half = t >= p.full;
+  const int f = half ? p.full + ((t - p.full) >> 1) : t, n = f / p.m_blocks;
+  return MxTile{n * 128, (f - n * p.m_blocks) * p.Mt + (half && ((t - p.full) & 1) ? p.Mt / 2 : 0), half ? p.Mt / 2 : p.Mt};
+}
 
 __host__ __device__ inline int mx_b_unit(int rows) { return rows * 128; }
 // rings of codes; with a split K range, the sums of the tile in their place afterwards, [row of x][128 channels]
@@ -158,40 +171,41 @@ struct RingCursor {
   }
 };
 
-template <typename T>
-__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
-  if (sizeof(T) == 4) return 0u;
-  T h[2] = {from_float<T>(a), from_float<T>(b)};
-  return *reinterpret_cast<const uint32_t*>(h);
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, __half) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, __nv_bfloat16) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_pair(float, float, float) { return 0u; }
 
-// 16 columns (rows of y) of a warp's 32 channels; dst: this lane's channel n in the first of them.  Where rows of y of a
-// 16-bit type start on 8 bytes, four lanes exchange their values of four rows, so that each then writes four channels of one row.
+// 16 columns (rows of y) of a warp's 32 channels.  wide: rows of a 16-bit type start on 8 bytes and all 32 channels exist: four lanes
+// exchange their values of four rows, so that each then writes four channels of one row; dst: the first of those in row lane & 3, live:
+// rows from there on.  Else dst: this lane's channel in the first row, live: rows of it.
 template <typename T>
-__device__ __forceinline__ void store_columns(T* dst, int64_t y_stride, const float* f, int vec, int n, int N, int live, int lane) {
+__device__ __forceinline__ void store_columns(T* dst, int64_t y_stride, const float* f, bool wide, int live, int lane) {
   const int j = lane & 3;
-  if (sizeof(T) == 4) {
-    if (n < N) {
-#pragma unroll
-      for (int c = 0; c < 16; ++c)
-        if (c < live) dst[c * y_stride] = from_float<T>(f[c]);
-    }
-  } else if (vec && n - lane + 32 <= N) {
+  if (sizeof(T) == 2 && wide) {
 #pragma unroll
     for (int c = 0; c < 16; c += 4) {
-      const uint32_t p01 = pack_pair<T>(f[c], f[c + 1]), p23 = pack_pair<T>(f[c + 2], f[c + 3]);
+      const uint32_t p01 = pack_pair(f[c], f[c + 1], T{}), p23 = pack_pair(f[c + 2], f[c + 3], T{});
       const uint32_t far = __shfl_xor_sync(0xffffffffu, j < 2 ? p23 : p01, 2), own = j < 2 ? p01 : p23;
       // rows (0, 1) or (2, 3) of channels j and j ^ 2, the lower channel first
       const uint32_t lo = j < 2 ? own : far, hi = j < 2 ? far : own;
       const uint32_t other = __shfl_xor_sync(0xffffffffu, __byte_perm(lo, hi, (j & 1) ? 0x5410 : 0x7632), 1);
       const uint32_t mine = __byte_perm(lo, hi, (j & 1) ? 0x7632 : 0x5410);       // this lane's row: channels (j, j + 2) or their neighbours'
       const uint32_t even = (j & 1) ? other : mine, odd = (j & 1) ? mine : other;
-      if (c + j < live) *reinterpret_cast<uint2*>(dst - j + (c + j) * y_stride) = make_uint2(__byte_perm(even, odd, 0x5410), __byte_perm(even, odd, 0x7632));
+      if (c < live) *reinterpret_cast<uint2*>(dst) = make_uint2(__byte_perm(even, odd, 0x5410), __byte_perm(even, odd, 0x7632));
+      dst += 4 * y_stride;
     }
-  } else if (n < N) {
+  } else {
 #pragma unroll
-    for (int c = 0; c < 16; ++c)
-      if (c < live) dst[c * y_stride] = from_float<T>(f[c]);
+    for (int c = 0; c < 16; ++c) {
+      if (c < live) *dst = from_float<T>(f[c]);
+      dst += y_stride;
+    }
   }
 }
 
@@ -285,12 +299,15 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 
   // warp 0: the first copies leave before the other warps are set up, the scale bytes of the weights before the weights themselves
   RingCursor ar;
-  int a_tile = first, a_chunk = c_begin;
+  int a_tile = first, a_chunk = c_begin, a_n0 = mx_tile(p, first).n0;
   auto send_a = [&]() {
-    tma_fill_2d(smem_u32(aring) + ar.stage * kMxATile, &a_map, a_full + 8 * ar.stage, KIND == 0 ? kMxATile : kMxACopied, a_chunk * 128,
-                a_tile / p.m_blocks * 128);
+    tma_fill_2d(smem_u32(aring) + ar.stage * kMxATile, &a_map, a_full + 8 * ar.stage, KIND == 0 ? kMxATile : kMxACopied, a_chunk * 128, a_n0);
     ar.sent(a_stages);
-    if (++a_chunk == c_end) { a_chunk = c_begin; a_tile += step; }
+    if (++a_chunk == c_end) {
+      a_chunk = c_begin;
+      a_tile += step;
+      a_n0 = mx_tile(p, a_tile).n0;
+    }
   };
   if (warp == 0) {
     if (lane == 0) {
@@ -308,7 +325,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    if (chunks > 0 && first < p.tiles) tma_fill_2d(smem_u32(sring), &sa_map, s_full, (uint32_t)((128 + p.rows * units) * 16), c_begin / Kd::CPS * 16, first / p.m_blocks * 128);
+    if (chunks > 0 && first < p.tiles) tma_fill_2d(smem_u32(sring), &sa_map, s_full, (uint32_t)((128 + (p.stack ? p.rows : mx_tile(p, first).Mt * units)) * 16), c_begin / Kd::CPS * 16, a_n0);
     if (chunks > 0)
       for (int i = 0; i < a_stages && a_tile < p.tiles; ++i) send_a();
   } else if (warp == 1) {
@@ -332,13 +349,16 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
     RingCursor r;
     for (int tile = first; tile < p.tiles && alive; tile += step) {
-      const int m0 = tile % p.m_blocks * p.Mt;
+      const MxTile at = mx_tile(p, tile);
+      const int boxes = at.Mt > p.box ? 2 : 1, bytes = p.stack ? b_unit : at.Mt * 128;
       for (int c0 = c_begin; c0 < c_end && alive; c0 += Kd::CPS)
         for (int u = units - 1; u >= 0 && alive; --u)
           for (int c = c0; c < min(c0 + Kd::CPS, c_end); ++c) {
             alive = mbar_wait_warp(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
             if (!alive) break;
-            tma_fill_3d(smem_u32(bring) + r.stage * b_unit, &b_map, b_full + 8 * r.stage, (uint32_t)b_unit, c * 128, m0, u);
+            const uint32_t dst = smem_u32(bring) + r.stage * b_unit;
+            tma_fill_3d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)bytes, c * 128, at.m0, u);
+            if (boxes == 2) tma_load_3d_elect(dst + p.box * 128, &b_map, b_full + 8 * r.stage, c * 128, at.m0 + p.box, u);
             r.sent(b_stages);
           }
     }
@@ -347,17 +367,20 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
     RingCursor r;
     for (int tile = first; tile < p.tiles && alive; tile += step) {
-      const int n0 = tile / p.m_blocks * 128, m0 = tile % p.m_blocks * p.Mt;
+      const MxTile at = mx_tile(p, tile);
+      const int boxes = at.Mt > p.box ? 2 : 1, bytes = (128 + (p.stack ? p.rows : at.Mt * units)) * 16;
       for (int s = 0; s < supers; ++s) {
         alive = mbar_wait_warp(s_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
         if (!alive) break;
         const uint32_t dst = smem_u32(sring) + r.stage * scale_tile, bar = s_full + 8 * r.stage;
         const int byte = (c_begin / Kd::CPS + s) * 16;
         if (tile != first || s != 0) {              // the very first by warp 0
-          expect_tx_elect(bar, (uint32_t)((128 + p.rows * units) * 16));
-          tma_load_2d_elect(dst, &sa_map, bar, byte, n0);
+          expect_tx_elect(bar, (uint32_t)bytes);
+          tma_load_2d_elect(dst, &sa_map, bar, byte, at.n0);
         }
-        for (int u = 0; u < units; ++u) tma_load_3d_elect(dst + (128 + u * p.b_cols * 32) * 16, &sb_map, bar, byte, m0, u);
+        for (int u = 0; u < units; ++u)
+          for (int b = 0; b < boxes; ++b)
+            tma_load_3d_elect(dst + (128 + u * p.b_cols * 32 + b * p.box) * 16, &sb_map, bar, byte, at.m0 + b * p.box, u);
         r.sent(kMxScaleStages);
       }
     }
@@ -368,13 +391,15 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     // operands are there is asked before this step's MMAs are issued.
     constexpr uint32_t DESC_HI = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);   // SBO 1024, version 1, 128-byte swizzle
     constexpr uint32_t LBO_FIELD = 1u << 16;
-    // operand types, N, scales in powers of two, M = 128
-    const uint32_t idesc = (KIND == 0 ? (1u << 7) | (1u << 10) : (5u << 7)) | ((uint32_t)(p.rows >> 3) << 17) | (1u << 23) | (1u << 27);
+    // operand types, scales in powers of two, M = 128; N with each tile
+    const uint32_t types = (KIND == 0 ? (1u << 7) | (1u << 10) : (5u << 7)) | (1u << 23) | (1u << 27);
     // The smallest pieces come first: while they are added up the sums are small, and so is what the additions drop.
     uint32_t as = 0, aph = 0, bs = 0, bph = 0, sets = 0, done = 0;               // sets, done: of all tiles so far
     bool ready = false, t_ready = false;
     for (int tile = first; tile < p.tiles && alive; tile += step, ++done) {
-      if (!PROMOTE && supers > 0) alive = mbar_wait_uniform(d_empty, (done & 1) ^ 1u, s_abort);
+      const uint32_t idesc = types | ((uint32_t)((tile < p.full ? p.rows : p.Mt / 2) >> 3) << 17);
+      const uint32_t db = p.d_bufs == 2 ? done & 1 : 0, dph = (p.d_bufs == 2 ? done >> 1 : done) & 1;
+      if (!PROMOTE && supers > 0) alive = mbar_wait_uniform(d_empty + 8 * db, dph ^ 1u, s_abort);
       for (int s = 0; s < supers && alive; ++s, ++sets) {
         const uint32_t tb = sets & 1, tph = (sets >> 1) & 1;
         uint32_t accumulate = !PROMOTE && s > 0;
@@ -382,7 +407,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         if (!t_ready) alive = alive && mbar_wait_uniform(t_full + 8 * tb, tph, s_abort);
         if (!alive) break;
         t_ready = false;
-        const uint32_t d = tmem_base + (PROMOTE ? tb * p.rows : 0);
+        const uint32_t d = tmem_base + (PROMOTE ? tb : db) * p.rows;
         const uint32_t sf = tmem_base + p.sf_col + tb * 4 * p.sf_group;
         const int n = min(Kd::CPS, chunks - s * Kd::CPS);
         for (int u = units - 1; u >= 0 && alive; --u) {
@@ -412,7 +437,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         }
         if (!alive) break;
         umma_commit(t_empty + 8 * tb);
-        if (PROMOTE || s + 1 == supers) umma_commit(d_full + 8 * (PROMOTE ? tb : 0));
+        if (PROMOTE || s + 1 == supers) umma_commit(d_full + 8 * (PROMOTE ? tb : db));
       }
     }
     if (!alive) {                                  // what was issued must end before the CTA does
@@ -453,14 +478,16 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   } else {
     // ---- sums: lane = output channel, column = row of x --------------------------------------------------
     if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int ch = (warp & 3) * 32 + lane, split = (p.Mt / 16 + 1) / 2 * 16;       // columns of the lower four warps
-    const int c_first = (warp >> 2) == 2 ? 0 : split, half = (warp >> 2) == 2 ? split : p.Mt - split;
-    const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + c_first;
+    const int ch = (warp & 3) * 32 + lane;
     const int copies = p.stack ? p.pieces : 1;                 // columns that belong to one row of x, Mt apart
-    float* sums = reinterpret_cast<float*>(smem) + c_first * 128 + ch;
     uint32_t sets = 0, done = 0;
     for (int tile = first; tile < p.tiles && alive; tile += step, ++done) {
-      const int n = tile / p.m_blocks * 128 + ch, m0 = tile % p.m_blocks * p.Mt + c_first;
+      const MxTile at = mx_tile(p, tile);
+      const int split = (at.Mt / 16 + 1) / 2 * 16;             // columns of the lower four warps
+      const int c_first = warp < 12 ? 0 : split, half = warp < 12 ? split : at.Mt - split;
+      const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + c_first;
+      float* sums = reinterpret_cast<float*>(smem) + c_first * 128 + ch;
+      const int n = at.n0 + ch, m0 = at.m0 + c_first;
       const bool direct = p.cluster == 1;
       const float b = direct && bias && n < p.N ? bias[n] : 0.f;
       const int live = n < p.N ? min(half, p.M - m0) : 0;      // this lane's columns that are rows of x
@@ -498,10 +525,13 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         }
       } else {
         // Not unrolled: code that a block runs once per tile comes from far away (unrolled, 16 columns took 1,000 cycles).
-        if (supers > 0) alive = mbar_wait_warp(d_full, done & 1, s_abort, nullptr);
+        const uint32_t db = p.d_bufs == 2 ? done & 1 : 0, dph = (p.d_bufs == 2 ? done >> 1 : done) & 1;
+        if (supers > 0) alive = mbar_wait_warp(d_full + 8 * db, dph, s_abort, nullptr);
         if (!alive) break;
         tc_fence_after();
-        T* out = dst;
+        const bool wide = sizeof(T) == 2 && p.y_vec && n - lane + 32 <= p.N;
+        T* out = wide ? y + (int64_t)(m0 + (lane & 3)) * y_stride + (n - (lane & 3)) : dst;
+        int left = wide ? p.M - m0 - (lane & 3) : n < p.N ? p.M - m0 : 0;
 #pragma unroll 1
         for (int c0 = 0; c0 < half; c0 += 16) {
           float f[16];
@@ -511,7 +541,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 #pragma unroll 1
             for (int q = copies - 1; q >= 0; --q) {
               uint32_t v[16];
-              tmem_ld16(taddr + q * p.Mt + c0, v);
+              tmem_ld16(taddr + db * p.rows + q * p.Mt + c0, v);
               tmem_ld_wait();
 #pragma unroll
               for (int j = 0; j < 16; ++j) f[j] += __uint_as_float(v[j]);
@@ -521,13 +551,14 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 #pragma unroll
             for (int j = 0; j < 16; ++j) sums[(c0 + j) * 128] = f[j];
           } else {
-            store_columns<T>(out, y_stride, f, vec, n, p.N, p.M - m0 - c0, lane);
+            store_columns<T>(out, y_stride, f, wide, left, lane);
             out += 16 * y_stride;
+            left -= 16;
           }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(d_empty);
+        if (lane == 0) mbar_arrive(d_empty + 8 * db);
       }
     }
   }
@@ -541,9 +572,9 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   if (p.cluster == 1) {
     if (*s_abort) {                                // a wait that ran out shows in the result
       for (int tile = first; tile < p.tiles; tile += step) {
-        const int n0 = tile / p.m_blocks * 128, m0 = tile % p.m_blocks * p.Mt;
-        for (int i = tid; i < p.Mt * 128; i += kMxTcThreads)
-          if (m0 + i / 128 < p.M && n0 + i % 128 < p.N) y[(int64_t)(m0 + i / 128) * y_stride + n0 + i % 128] = from_float<T>(__int_as_float(0x7FC00000));
+        const MxTile at = mx_tile(p, tile);
+        for (int i = tid; i < at.Mt * 128; i += kMxTcThreads)
+          if (at.m0 + i / 128 < p.M && at.n0 + i % 128 < p.N) y[(int64_t)(at.m0 + i / 128) * y_stride + at.n0 + i % 128] = from_float<T>(__int_as_float(0x7FC00000));
       }
     }
     return;
@@ -555,7 +586,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
   if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int n0 = first / p.m_blocks * 128, m0 = first % p.m_blocks * p.Mt, rows = min(p.Mt, p.M - m0);
+  const int n0 = mx_tile(p, first).n0, m0 = mx_tile(p, first).m0, rows = min(p.Mt, p.M - m0);
   for (int r = rank + warp * p.cluster; r < rows; r += (kMxTcThreads / 32) * p.cluster) {
     T* dst = y + (int64_t)(m0 + r) * y_stride + n0;
     if (vec && n0 + lane * 4 + 4 <= p.N) {                     // rows of y start on four values: a lane takes four channels
@@ -669,26 +700,59 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   p.N = g.N; p.M = g.M;
   p.pieces = KIND == 1 ? PieceCount<T>::N : 1;
   p.n_chunks = (g.K + Kd::CHUNK - 1) / Kd::CHUNK;
-  const int n_super = (g.K + kMxSuper - 1) / kMxSuper, row_blocks = (g.N + 127) / 128;
-  // rows of x per tile: the sums of a tile and the scale words have to fit into 512 columns
-  const int widest = PROMOTE ? 128 : 256;
-  const int stacked = p.pieces == 1 ? widest : (PROMOTE ? 160 : 256) / p.pieces / 16 * 16;
+  const int n_super = (g.K + kMxSuper - 1) / kMxSuper, row_blocks = (g.N + 127) / 128, n_sms = props.n_sms;
+  // Rows of x per tile (Mt): the sums of a tile and the scale words have to fit into 512 columns.
+  const int widest = PROMOTE ? 128 : 256, stacked = p.pieces == 1 ? 0 : (PROMOTE ? 160 : 256) / p.pieces / 16 * 16;
   p.stack = g.M <= stacked;
-  const int most = p.stack ? stacked : widest;
-  p.Mt = g.M >= most ? most : (g.M + 15) / 16 * 16;
-  p.rows = p.stack ? p.Mt * p.pieces : p.Mt;
-  p.b_cols = ((p.rows + 31) / 32 + 3) / 4 * 4;
-  p.sf_group = 4 + p.b_cols * (p.stack ? 1 : p.pieces);
-  p.sf_col = PROMOTE ? 2 * p.rows : p.rows;
-  p.tmem_cols = 32;
-  while (p.tmem_cols < p.sf_col + 8 * p.sf_group) p.tmem_cols <<= 1;
-  if (p.tmem_cols > 512) return set_error(AIQ_ERR_SHAPE, "mx_tc: %d columns of tensor memory", p.tmem_cols);
-  p.m_blocks = (g.M + p.Mt - 1) / p.Mt;
-  if ((int64_t)row_blocks * p.m_blocks > 0x7FFFFFFF) return set_error(AIQ_ERR_SHAPE, "mx_tc: too many tiles");
-  p.tiles = row_blocks * p.m_blocks;
-  const int splits = props.n_sms / p.tiles;
-  p.cluster = 1;
-  while (p.cluster * 2 <= splits && p.cluster * 2 <= n_super && p.cluster < 8) p.cluster *= 2;
+  auto shape = [&](MxTcParams& q, int Mt) {
+    q.Mt = Mt;
+    q.rows = q.stack ? Mt * q.pieces : Mt;
+    q.b_cols = ((q.rows + 31) / 32 + 3) / 4 * 4;
+    q.sf_group = 4 + q.b_cols * (q.stack ? 1 : q.pieces);
+    q.m_blocks = (g.M + Mt - 1) / Mt;
+    const int64_t tiles = (int64_t)row_blocks * q.m_blocks;
+    if (tiles > 0x3FFFFFFF) return false;
+    q.full = q.tiles = (int)tiles;
+    q.box = Mt;
+    q.cluster = 1;
+    while (q.cluster * 2 <= n_sms / q.tiles && q.cluster * 2 <= n_super && q.cluster < 8) q.cluster *= 2;
+    // The tiles behind the last whole round over the SMs, where they are at most half a round, are cut in half.
+    const int rest = q.tiles % n_sms;
+    if (!q.stack && q.tiles > n_sms && rest > 0 && rest * 2 <= n_sms && Mt % 32 == 0) {
+      q.full = q.tiles - rest;
+      q.tiles = q.full + 2 * rest;
+      q.box = Mt / 2;
+    }
+    q.d_bufs = PROMOTE || (tiles > n_sms && 2 * q.rows + 8 * q.sf_group <= 512) ? 2 : 1;
+    q.sf_col = q.d_bufs * q.rows;
+    q.tmem_cols = 32;
+    while (q.tmem_cols < q.sf_col + 8 * q.sf_group) q.tmem_cols <<= 1;
+    return q.tmem_cols <= 512;
+  };
+  if (p.stack) {
+    if (!shape(p, (g.M + 15) / 16 * 16)) return set_error(AIQ_ERR_SHAPE, "mx_tc: N=%d M=%d", g.N, g.M);
+  } else {
+    // The width of the tiles decides how evenly they go into rounds over the SMs; a wide tile reads fewer operand bytes per product,
+    // a narrow one leaves room for two sets of sums.  On the device, 8192 x 8192, 2,048 rows, Mt 256 | 192 | 160 | 128: both
+    // microscaled 65 | 61 | 65 | 68 us, bfloat16 207 | 219 | 227 | 240, half 367 | 351 | 356 | 360; 4096 x 4096, 2,048 rows, both
+    // microscaled 23.5 | 21.4 | 21.6 | 23.7; 1,024 rows bfloat16 37 | 44 | 43 | 40 (one round of 128 tiles at 256).
+    double best = 0;
+    bool found = false;
+    for (int Mt = (g.M + 15) / 16 * 16 < widest ? (g.M + 15) / 16 * 16 : widest; Mt >= 64; Mt = (Mt - 1) / 32 * 32) {
+      MxTcParams q = p;
+      if (!shape(q, Mt)) continue;
+      const int rest = q.full == q.tiles ? q.tiles % n_sms : 0;
+      const double rounds = q.full == q.tiles ? q.tiles / n_sms + (rest ? 1.0 : 0.0) : q.full / n_sms + 0.55;
+      // columns' worth of time: KIND 0 a fixed part, and the sums' way out where it is not covered; KIND 1 the MMAs of at least 160
+      const double tile = KIND == 0 ? Mt + 40 + (q.d_bufs == 1 ? 40 : 0) : Mt > 160 ? Mt : 160;
+      const double cost = rounds * tile / q.cluster + (q.cluster > 1 ? 25 : 0);
+      if (!found || cost < best) { best = cost; p = q; found = true; }
+      if (PROMOTE || Mt <= 128) break;
+    }
+    if (!found) {
+      if (!shape(p, g.M < 64 ? (g.M + 15) / 16 * 16 : 64)) return set_error(AIQ_ERR_SHAPE, "mx_tc: N=%d M=%d", g.N, g.M);
+    }
+  }
   p.supers_per_split = (n_super + p.cluster - 1) / p.cluster;
   const int chunks = p.supers_per_split * Kd::CPS, units = p.stack ? 1 : p.pieces;
   p.a_stages = units > 1 ? Kd::CPS : 2;                        // the pieces of one set of chunks read the same weights
@@ -721,10 +785,10 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
 
     const uint8_t* scales = KIND == 0 ? g.x_scales : workspace + P * M * x_row;
     const cuuint64_t dims[3] = {x_row, M, P}, strides[2] = {x_row, x_row * M};
-    const cuuint32_t box[3] = {128, (cuuint32_t)p.Mt, (cuuint32_t)(p.stack ? P : 1)};
+    const cuuint32_t box[3] = {128, (cuuint32_t)p.box, (cuuint32_t)(p.stack ? P : 1)};
     if (aiq_status_t st = encode(enc, &b_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
     const cuuint64_t sdims[3] = {s_row, M, P}, sstrides[2] = {s_row, s_row * M};
-    const cuuint32_t sbox[3] = {16, (cuuint32_t)p.Mt, (cuuint32_t)(p.stack ? P : 1)};
+    const cuuint32_t sbox[3] = {16, (cuuint32_t)p.box, (cuuint32_t)(p.stack ? P : 1)};
     if (aiq_status_t st = encode(enc, &sb_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, 3, sdims, sstrides, sbox, CU_TENSOR_MAP_SWIZZLE_NONE))
       return st;
   }
