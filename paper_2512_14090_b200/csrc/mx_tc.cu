@@ -171,41 +171,15 @@ struct RingCursor {
   }
 };
 
-__device__ __forceinline__ uint32_t pack_pair(float a, float b, __half) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t pack_pair(float a, float b, __nv_bfloat16) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ uint32_t pack_pair(float, float, float) { return 0u; }
-
-// 16 columns (rows of y) of a warp's 32 channels.  wide: rows of a 16-bit type start on 8 bytes and all 32 channels exist: four lanes
-// exchange their values of four rows, so that each then writes four channels of one row; dst: the first of those in row lane & 3, live:
-// rows from there on.  Else dst: this lane's channel in the first row, live: rows of it.
+// 16 columns of a warp's 32 channels: 16 rows of y, a run of 32 values each.  dst: this lane's channel in the first row; live: rows
+// left.  (Exchanging values among four lanes, so that each writes 8 bytes, costs more instructions than it saves: 850 cycles for 16
+// columns instead of 700.)
 template <typename T>
-__device__ __forceinline__ void store_columns(T* dst, int64_t y_stride, const float* f, bool wide, int live, int lane) {
-  const int j = lane & 3;
-  if (sizeof(T) == 2 && wide) {
+__device__ __forceinline__ void store_columns(T* dst, int64_t y_stride, const float* f, int live) {
 #pragma unroll
-    for (int c = 0; c < 16; c += 4) {
-      const uint32_t p01 = pack_pair(f[c], f[c + 1], T{}), p23 = pack_pair(f[c + 2], f[c + 3], T{});
-      const uint32_t far = __shfl_xor_sync(0xffffffffu, j < 2 ? p23 : p01, 2), own = j < 2 ? p01 : p23;
-      // rows (0, 1) or (2, 3) of channels j and j ^ 2, the lower channel first
-      const uint32_t lo = j < 2 ? own : far, hi = j < 2 ? far : own;
-      const uint32_t other = __shfl_xor_sync(0xffffffffu, __byte_perm(lo, hi, (j & 1) ? 0x5410 : 0x7632), 1);
-      const uint32_t mine = __byte_perm(lo, hi, (j & 1) ? 0x7632 : 0x5410);       // this lane's row: channels (j, j + 2) or their neighbours'
-      const uint32_t even = (j & 1) ? other : mine, odd = (j & 1) ? mine : other;
-      if (c < live) *reinterpret_cast<uint2*>(dst) = make_uint2(__byte_perm(even, odd, 0x5410), __byte_perm(even, odd, 0x7632));
-      dst += 4 * y_stride;
-    }
-  } else {
-#pragma unroll
-    for (int c = 0; c < 16; ++c) {
-      if (c < live) *dst = from_float<T>(f[c]);
-      dst += y_stride;
-    }
+  for (int c = 0; c < 16; ++c) {
+    if (c < live) *dst = from_float<T>(f[c]);
+    dst += y_stride;
   }
 }
 
@@ -529,9 +503,8 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         if (supers > 0) alive = mbar_wait_warp(d_full + 8 * db, dph, s_abort, nullptr);
         if (!alive) break;
         tc_fence_after();
-        const bool wide = sizeof(T) == 2 && p.y_vec && n - lane + 32 <= p.N;
-        T* out = wide ? y + (int64_t)(m0 + (lane & 3)) * y_stride + (n - (lane & 3)) : dst;
-        int left = wide ? p.M - m0 - (lane & 3) : n < p.N ? p.M - m0 : 0;
+        T* out = dst;
+        int left = n < p.N ? p.M - m0 : 0;
 #pragma unroll 1
         for (int c0 = 0; c0 < half; c0 += 16) {
           float f[16];
@@ -551,7 +524,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 #pragma unroll
             for (int j = 0; j < 16; ++j) sums[(c0 + j) * 128] = f[j];
           } else {
-            store_columns<T>(out, y_stride, f, wide, left, lane);
+            store_columns<T>(out, y_stride, f, left);
             out += 16 * y_stride;
             left -= 16;
           }
