@@ -51,7 +51,8 @@ struct MxTcParams {
   int stack;                // 1: the pieces' rows are one operand
   int rows;                 // rows of a B operand: Mt, stacked pieces * Mt
   int n_chunks, supers_per_split;
-  int cluster;
+  int cluster, cluster_log2;
+  int push;                 // bytes for sums that the cluster's CTAs write into each other's shared memory; 0: read from it afterwards
   int m_blocks, tiles;      // tiles: row blocks * m_blocks, then the halves of some of them:
   int full;                 // tiles from this one on are halves of tiles (Mt / 2 rows of x), two for each
   int box;                  // rows of x per copy: Mt, or Mt / 2 where there are halves
@@ -73,10 +74,10 @@ __device__ __forceinline__ MxTile mx_tile(const MxTcParams& p, int t) {
 }
 
 __host__ __device__ inline int mx_b_unit(int rows) { return rows * 128; }
-// rings of codes; with a split K range, the sums of the tile in their place afterwards, [row of x][128 channels]
+// rings of codes; with a split K range the sums of the tile, [row of x][128 channels], in their place afterwards or behind them
 __host__ __device__ inline int mx_ring_bytes(const MxTcParams& p) {
-  const int rings = p.a_stages * kMxATile + p.b_stages * mx_b_unit(p.rows), sums = p.cluster > 1 ? p.Mt * 128 * 4 : 0;
-  return rings > sums ? rings : sums;
+  const int rings = p.a_stages * kMxATile + p.b_stages * mx_b_unit(p.rows), sums = p.cluster > 1 && !p.push ? p.Mt * 128 * 4 : 0;
+  return (rings > sums ? rings : sums) + p.push;
 }
 __host__ __device__ inline int mx_scale_tile(const MxTcParams& p) { return (128 + p.b_cols * 32 * (p.stack ? 1 : p.pieces)) * 16; }
 inline int mx_smem_bytes(const MxTcParams& p) {
@@ -250,8 +251,8 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   // Broadcast, so that the compiler sees values that are the same in the whole warp and keeps what the tensor-core instructions take
   // in uniform registers: with plain tid >> 5 and the address as it lies in shared memory an MMA took 180 to 250 cycles to issue.
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-  const int rank = blockIdx.x % p.cluster;
-  const int first = blockIdx.x / p.cluster, step = gridDim.x / p.cluster;      // this CTA's tiles
+  const int rank = blockIdx.x & (p.cluster - 1);
+  const int first = blockIdx.x >> p.cluster_log2, step = gridDim.x >> p.cluster_log2;      // this CTA's tiles
   const int a_stages = p.a_stages, b_stages = p.b_stages, units = p.stack ? 1 : p.pieces;
   const int b_unit = mx_b_unit(p.rows), scale_tile = mx_scale_tile(p);
   const int c_begin = min(p.n_chunks, rank * p.supers_per_split * Kd::CPS);
@@ -284,24 +285,16 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     }
   };
   if (warp == 0) {
-    if (lane == 0) {
-      for (int i = 0; i < a_stages; ++i) { mbar_init(a_full + 8 * i, 1); mbar_init(a_empty + 8 * i, 1); }
-      for (int i = 0; i < b_stages; ++i) { mbar_init(b_full + 8 * i, 1); mbar_init(b_empty + 8 * i, 1); }
-      for (int i = 0; i < kMxScaleStages; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_empty + 8 * i, 4); }
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(t_full + 8 * i, 4);
-        mbar_init(t_empty + 8 * i, 1);
-        mbar_init(d_full + 8 * i, 1);
-        mbar_init(d_empty + 8 * i, 8);
-      }
-      mbar_init(retired, 1);
-      *s_abort = 0;
-      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
+    // arrivals: four warps for scale bytes read and words written, eight for sums read, one for everything else
+    const int rings = 2 * (a_stages + b_stages) + kMxScaleStages;
+    for (int i = lane; i < rings + kMxScaleStages + 9; i += 32)
+      mbar_init(a_full + 8 * i, i >= rings && i < rings + kMxScaleStages + 2 ? 4 : i >= rings + kMxScaleStages + 6 && i < rings + kMxScaleStages + 8 ? 8 : 1);
+    if (lane == 0) *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
     if (chunks > 0 && first < p.tiles) tma_fill_2d(smem_u32(sring), &sa_map, s_full, (uint32_t)((128 + (p.stack ? p.rows : mx_tile(p, first).Mt * units)) * 16), c_begin / Kd::CPS * 16, a_n0);
     if (chunks > 0)
-      for (int i = 0; i < a_stages && a_tile < p.tiles; ++i) send_a();
+      for (int i = 0; i < 2 && a_tile < p.tiles; ++i) send_a();
   } else if (warp == 1) {
     tmem_alloc(smem_u32(s_tmem), (uint32_t)p.tmem_cols);
     tmem_relinquish();
@@ -309,6 +302,8 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // Before a CTA writes into another's shared memory, that one has to have started: arrived here, waited for at the first write.
+  if (p.push) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   const uint32_t tmem_base = __shfl_sync(0xffffffffu, *s_tmem, 0);
   bool alive = true;
 
@@ -452,6 +447,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   } else {
     // ---- sums: lane = output channel, column = row of x --------------------------------------------------
     if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (p.push) asm volatile("barrier.cluster.wait;" ::: "memory");
     const int ch = (warp & 3) * 32 + lane;
     const int copies = p.stack ? p.pieces : 1;                 // columns that belong to one row of x, Mt apart
     uint32_t sets = 0, done = 0;
@@ -461,6 +457,13 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       const int c_first = warp < 12 ? 0 : split, half = warp < 12 ? split : at.Mt - split;
       const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + c_first;
       float* sums = reinterpret_cast<float*>(smem) + c_first * 128 + ch;
+      // push: row r of the tile belongs to CTA r mod cluster, which gets a copy from every CTA: [CTA][row / cluster][128]
+      const uint32_t mine = smem_u32(smem) + mx_ring_bytes(p) - p.push + ((rank * p.Mt) >> p.cluster_log2) * 512 + ch * 4;
+      auto push = [&](int r, float v) {
+        uint32_t to;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(mine + (uint32_t)(r >> p.cluster_log2) * 512), "r"(r & (p.cluster - 1)));
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v) : "memory");
+      };
       const int n = at.n0 + ch, m0 = at.m0 + c_first;
       const bool direct = p.cluster == 1;
       const float b = direct && bias && n < p.N ? bias[n] : 0.f;
@@ -491,11 +494,20 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
           __syncwarp();
           if (lane == 0) mbar_arrive(d_empty + 8 * tb);
         }
+        if (direct) {
 #pragma unroll
-        for (int c = 0; c < 64; ++c) {
-          if (c >= half) break;
-          if (!direct) sums[c * 128] = acc[c];
-          else if (c < live && alive) dst[c * y_stride] = from_float<T>(acc[c] + b);
+          for (int c = 0; c < 64; ++c) {
+            if (c < live && alive) *dst = from_float<T>(acc[c] + b);
+            dst += y_stride;
+          }
+        } else if (p.push) {
+#pragma unroll
+          for (int c = 0; c < 32; ++c)                         // Mt is 64 at most
+            if (c < half) push(c_first + c, acc[c]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c < half) sums[c * 128] = acc[c];
         }
       } else {
         // Not unrolled: code that a block runs once per tile comes from far away (unrolled, 16 columns took 1,000 cycles).
@@ -520,7 +532,10 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
               for (int j = 0; j < 16; ++j) f[j] += __uint_as_float(v[j]);
             }
           }
-          if (!direct) {
+          if (p.push) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) push(c_first + c0 + j, f[j]);
+          } else if (!direct) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) sums[(c0 + j) * 128] = f[j];
           } else {
@@ -554,55 +569,72 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   }
 
   // ---- sums of the cluster -> y, a row of 128 channels per warp -------------------------------------
-  if (*s_abort)
-    for (int i = tid; i < p.Mt * 128; i += kMxTcThreads) reinterpret_cast<float*>(smem)[i] = __int_as_float(0x7FC00000);
+  if (p.push && warp < 8) asm volatile("barrier.cluster.wait;" ::: "memory");
+  if (*s_abort) {
+    if (p.push) {                                  // the last word on every copy that this CTA owes the others
+      const uint32_t mine = smem_u32(smem) + mx_ring_bytes(p) - p.push + ((rank * p.Mt) >> p.cluster_log2) * 512;
+      for (int i = tid; i < p.Mt * 128; i += kMxTcThreads) {
+        uint32_t to;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(mine + (uint32_t)((i >> 7) >> p.cluster_log2) * 512 + (i & 127) * 4), "r"((i >> 7) & (p.cluster - 1)));
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(__int_as_float(0x7FC00000)) : "memory");
+      }
+    } else {
+      for (int i = tid; i < p.Mt * 128; i += kMxTcThreads) reinterpret_cast<float*>(smem)[i] = __int_as_float(0x7FC00000);
+    }
+  }
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
   if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int n0 = mx_tile(p, first).n0, m0 = mx_tile(p, first).m0, rows = min(p.Mt, p.M - m0);
+  const MxTile at = mx_tile(p, first);
+  const int n0 = at.n0, m0 = at.m0, rows = min(p.Mt, p.M - m0);
+  const uint32_t copy = ((uint32_t)p.Mt >> p.cluster_log2) * 512;       // push: bytes of one CTA's sums here
   for (int r = rank + warp * p.cluster; r < rows; r += (kMxTcThreads / 32) * p.cluster) {
     T* dst = y + (int64_t)(m0 + r) * y_stride + n0;
-    if (vec && n0 + lane * 4 + 4 <= p.N) {                     // rows of y start on four values: a lane takes four channels
-      const uint32_t mine = smem_u32(smem) + (uint32_t)(r * 128 + lane * 4) * 4;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const uint32_t here = p.push ? smem_u32(smem) + mx_ring_bytes(p) - p.push + (uint32_t)(r >> p.cluster_log2) * 512 : smem_u32(smem) + (uint32_t)r * 512;
+    // lane: four neighbouring channels where rows of y start on four values, else every 32nd
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (p.y_vec) {
       for (int q = 0; q < p.cluster; ++q) {
-        uint32_t theirs;
         float4 part;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(theirs) : "r"(mine), "r"(q));
-        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                     : "=f"(part.x), "=f"(part.y), "=f"(part.z), "=f"(part.w) : "r"(theirs) : "memory");
-        sum.x += part.x; sum.y += part.y; sum.z += part.z; sum.w += part.w;
+        uint32_t from;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(here + lane * 16 + (p.push ? q * copy : 0u)), "r"(p.push ? rank : q));
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(part.x), "=f"(part.y), "=f"(part.z), "=f"(part.w) : "r"(from) : "memory");
+        sum[0] += part.x; sum[1] += part.y; sum[2] += part.z; sum[3] += part.w;
       }
-      if (bias) {
-        const float* b = bias + n0 + lane * 4;
-        sum.x += b[0]; sum.y += b[1]; sum.z += b[2]; sum.w += b[3];
+    } else {
+      for (int q = 0; q < p.cluster; ++q) {
+        float part[4];
+        uint32_t from;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(from) : "r"(here + lane * 4 + (p.push ? q * copy : 0u)), "r"(p.push ? rank : q));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[j]) : "r"(from + j * 128) : "memory");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += part[j];
       }
+    }
+    const int c0 = p.y_vec ? lane * 4 : lane, c_step = p.y_vec ? 1 : 32;
+    if (bias) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n0 + c0 + j * c_step < p.N) sum[j] += bias[n0 + c0 + j * c_step];
+    }
+    if (p.y_vec && n0 + c0 + 4 <= p.N) {
       if (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(dst + lane * 4) = sum;
+        *reinterpret_cast<float4*>(dst + c0) = make_float4(sum[0], sum[1], sum[2], sum[3]);
       } else {
-        T h[4] = {from_float<T>(sum.x), from_float<T>(sum.y), from_float<T>(sum.z), from_float<T>(sum.w)};
-        *reinterpret_cast<uint2*>(dst + lane * 4) = *reinterpret_cast<const uint2*>(h);
+        T h[4] = {from_float<T>(sum[0]), from_float<T>(sum[1]), from_float<T>(sum[2]), from_float<T>(sum[3])};
+        *reinterpret_cast<uint2*>(dst + c0) = *reinterpret_cast<const uint2*>(h);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int ch = vec ? lane * 4 + j : lane + 32 * j;
-        if (n0 + ch >= p.N) continue;
-        const uint32_t mine = smem_u32(smem) + (uint32_t)(r * 128 + ch) * 4;
-        float sum = 0.f;
-        for (int q = 0; q < p.cluster; ++q) {
-          uint32_t theirs;
-          float part;
-          asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(theirs) : "r"(mine), "r"(q));
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(theirs) : "memory");
-          sum += part;
-        }
-        dst[ch] = from_float<T>(sum + (bias ? bias[n0 + ch] : 0.f));
-      }
+      for (int j = 0; j < 4; ++j)
+        if (n0 + c0 + j * c_step < p.N) dst[c0 + j * c_step] = from_float<T>(sum[j]);
     }
   }
-  asm volatile("barrier.cluster.arrive.release;" ::: "memory");      // no CTA leaves while another reads its sums
-  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  if (!p.push) {                                   // no CTA leaves while another reads its sums
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -726,6 +758,8 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
       if (!shape(p, g.M < 64 ? (g.M + 15) / 16 * 16 : 64)) return set_error(AIQ_ERR_SHAPE, "mx_tc: N=%d M=%d", g.N, g.M);
     }
   }
+  while ((1 << p.cluster_log2) < p.cluster) ++p.cluster_log2;
+  p.push = p.cluster > 1 && p.Mt <= 64 ? p.Mt * 512 : 0;       // Mt is a multiple of 16, the cluster has 2, 4 or 8 CTAs
   p.supers_per_split = (n_super + p.cluster - 1) / p.cluster;
   const int chunks = p.supers_per_split * Kd::CPS, units = p.stack ? 1 : p.pieces;
   p.a_stages = units > 1 ? Kd::CPS : 2;                        // the pieces of one set of chunks read the same weights
