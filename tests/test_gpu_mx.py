@@ -64,6 +64,28 @@ def test_dequantize(dtype, rows, k, pad):
     assert (got[:, k:] == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("rows,k,step", [(3, 700, 1), (5, 1031, 0), (2, 8, 1), (9, 25, 2), (300, 4000, 3)])
+def test_rows_that_start_anywhere(dtype, rows, k, step):
+    """Every offset of a row's start from a 16- or 32-byte boundary, reading and writing; nothing beside the rows is touched."""
+    b, dt = binding(), TYPES[dtype]
+    g = torch.Generator().manual_seed(k)
+    for skip in range(9):
+        wide = (torch.randn((rows, k + skip + step), generator=g) * 3).to(dt).cuda()
+        x = wide[:, skip:skip + k]
+        codes, scales = held(x)
+        ref_codes, ref_scales = X.quantize(x[:3].cpu().double().numpy())
+        assert np.array_equal(codes[:3].cpu().numpy(), ref_codes) and np.array_equal(scales[:3].cpu().numpy(), ref_scales)
+        plain_codes, plain_scales = held(x.contiguous())
+        assert torch.equal(codes, plain_codes) and torch.equal(scales, plain_scales)
+        out = torch.full_like(wide, 7.0)
+        b.aiq_mx_dequantize(codes, scales, out[:, skip:skip + k])
+        ref = torch.from_numpy(values(codes, scales, k).astype(np.float32)).to(dt)
+        assert torch.equal(out[:, skip:skip + k].cpu(), ref)
+        out[:, skip:skip + k] = 7.0
+        assert (out == 7.0).all()
+
+
 def test_every_code_and_scale():
     """All 256 bytes of codes under all 256 scale bytes."""
     b = binding()
