@@ -280,15 +280,13 @@ def _mx_plan(key, check, *args):
 _mx_plans = {}
 
 
-def _mx_stream(stream, *tensors):
-    """The launch goes to the current device (its current stream): every tensor has to lie there."""
+def _mx_stream(stream, device, same):
+    """The launch goes to the current device (its current stream): `device`, where `same` says that every tensor lies."""
     if _raw_stream is None:
         _stream()
     current, raw = _raw_stream
-    device = current()
-    for t in tensors:                                   # -1: not a CUDA tensor
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"expected every tensor on the current device, cuda:{device}, not {t.device}")
+    if not same or device != current():                     # -1: not a CUDA tensor
+        raise ValueError(f"expected every tensor on the current device, cuda:{current()}")
     return raw(device) if stream is None else stream.cuda_stream
 
 
@@ -362,7 +360,8 @@ def aiq_mx_quantize(x, codes_out, scales_out, stream=None):
     key = (codes_out.shape, scales_out.shape, x.shape, x.stride(), x.dtype, codes_out.dtype, scales_out.dtype,
            codes_out.is_contiguous(), scales_out.is_contiguous())
     dtype, rows, k, stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_values, codes_out, scales_out, x)
-    s = _mx_stream(stream, x, codes_out, scales_out)
+    d = x.get_device()
+    s = _mx_stream(stream, d, d == codes_out.get_device() == scales_out.get_device())
     status = lib.aiq_mx_quantize(x.data_ptr(), dtype, rows, k, stride, codes_out.data_ptr(), scales_out.data_ptr(), s)
     if status:
         _check(status)
@@ -372,7 +371,8 @@ def aiq_mx_dequantize(codes, scales, y, stream=None):
     """codes, scales -> y [rows][K] float32, float16 or bfloat16."""
     key = (codes.shape, scales.shape, y.shape, y.stride(), y.dtype, codes.dtype, scales.dtype, codes.is_contiguous(), scales.is_contiguous())
     dtype, rows, k, stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_values, codes, scales, y)
-    s = _mx_stream(stream, y, codes, scales)
+    d = y.get_device()
+    s = _mx_stream(stream, d, d == codes.get_device() == scales.get_device())
     status = lib.aiq_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, dtype, y.data_ptr(), stride, s)
     if status:
         _check(status)
@@ -387,7 +387,9 @@ def aiq_mx_linear(codes, scales, bias, x, y, workspace=None, stream=None):
     key = (codes.shape, scales.shape, x.shape, y.shape, x.stride(), y.stride(), x.dtype, y.dtype, codes.dtype, scales.dtype,
            codes.is_contiguous(), scales.is_contiguous(), (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None)
     n, k, dtype, m, x_stride, y_stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_linear, codes, scales, bias, x, y)
-    s = _mx_stream(stream, x, y, codes, scales, bias, workspace)
+    d = x.get_device()
+    s = _mx_stream(stream, d, d == y.get_device() == codes.get_device() == scales.get_device()
+                   and (bias is None or bias.get_device() == d) and (workspace is None or workspace.get_device() == d))
     ws, size = (_dev(workspace), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
     status = lib.aiq_mx_linear(codes.data_ptr(), scales.data_ptr(), bias.data_ptr() if bias is not None else None, n, k, x.data_ptr(), dtype,
                                m, x_stride, y.data_ptr(), y_stride, ws, size, s)
@@ -401,7 +403,9 @@ def aiq_mx_matmul(a_codes, a_scales, b_codes, b_scales, bias, K, y, stream=None)
            b_codes.dtype, b_scales.dtype, a_codes.is_contiguous(), a_scales.is_contiguous(), b_codes.is_contiguous(),
            b_scales.is_contiguous(), (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None)
     m, n, dtype, y_stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_matmul, a_codes, a_scales, b_codes, b_scales, bias, y, int(K))
-    s = _mx_stream(stream, y, a_codes, a_scales, b_codes, b_scales, bias)
+    d = y.get_device()
+    s = _mx_stream(stream, d, d == a_codes.get_device() == a_scales.get_device() == b_codes.get_device() == b_scales.get_device()
+                   and (bias is None or bias.get_device() == d))
     status = lib.aiq_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), m, b_codes.data_ptr(), b_scales.data_ptr(), n,
                                bias.data_ptr() if bias is not None else None, int(K), y.data_ptr(), dtype, y_stride, s)
     if status:
