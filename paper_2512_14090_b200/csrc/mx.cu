@@ -507,13 +507,14 @@ extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales,
 // Whether the kernel for few rows and small matrices beats the tensor-core kernel, whose time below 2^22 products is its chain of
 // set-up, first loads and last stores.  On the device, rows | tensor cores (linear layer: with its pre-pass, a second launch):
 //   linear, bf16     1 row: 1280 x 320 2.6 | 7.0 us, 2000 x 2000 4.7 | 8.2, 4096 x 4096 9.2 | 9.7, 8192 x 8192 28 | 15.5
-//                    4 rows: 724 x 724 4.9 | 7.5, 2000 x 2000 8.4 | 8.2;  8 rows, 724 x 724 5.6 | 7.4;  16 rows 9.4 | 7.6
+//                    4 rows: 724 x 724 4.9 | 7.5, 2000 x 2000 8.4 | 8.2;  8 rows, 724 x 724 5.6 | 6.9, 720 x 720 4.3 | 7.0;
+//                    16 rows, 724 x 724 (rows that do not start on 16 bytes) 9.4 | 7.0, 720 x 720 5.4 | 7.0, 300 x 2000 6.9 | 7.2
 //   both microscaled 1 row: 2000 x 2000 4.8 | 6.3, 4096 x 4096 10.0 | 7.6;  8 rows, 300 x 300 3.2 | 4.9;  4 rows, 2000 x 2000 8.0 | 6.4
 static bool mx_rows_pay(int N, int K, int M, int log2_most) { return (double)N * K * M <= (double)(1ll << log2_most); }
 
 extern "C" size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype) {
   if (N <= 0 || K <= 0 || M <= 0 || !aiq::mx_dtype_ok(dtype)) return 0;
-  return mx_rows_pay(N, K, M, M <= 4 ? 24 : 22) ? 0 : aiq::mx_tc_workspace_bytes(K, M, dtype);
+  return mx_rows_pay(N, K, M, M <= 4 ? 24 : K % 8 == 0 ? 23 : 22) ? 0 : aiq::mx_tc_workspace_bytes(K, M, dtype);
 }
 
 extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,

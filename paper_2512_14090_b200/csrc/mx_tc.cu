@@ -641,27 +641,38 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 // x -> eight-bit pieces, for a large batch
 // ---------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 256;
+constexpr int kSplitWords = 2;               // words of eight values per lane
 
+// A warp takes 512 values of one row, a lane eight at a time.  Bound by memory: 2,048 x 8192 bfloat16 17.5 us with a division for every
+// word.
 template <typename T>
 __global__ void __launch_bounds__(kSplitThreads)
-mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int M, int vec, FastDiv words, int scale_row, uint64_t units,
+mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int64_t M, int vec, uint64_t segments, uint32_t per_row, int words, int scale_row,
                   uint2* __restrict__ planes, uint8_t* __restrict__ scales) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const uint64_t u = (uint64_t)blockIdx.x * kSplitThreads + threadIdx.x;
-  const bool live = u < units;
-  const uint32_t row = live ? (uint32_t)(u < (1ull << 31) ? words.div((uint32_t)u) : u / words.d) : 0u;
-  const uint32_t word = live ? (uint32_t)(u - (uint64_t)row * words.d) : 0u;
-  float f[8];
-  load_x(x + (int64_t)row * x_stride, (int)word * 8, live ? K : 0, vec, f);
-  uint8_t* sr = scales + (int64_t)row * scale_row;
-  const int64_t piece_words = (int64_t)M * words.d, piece_scales = (int64_t)M * scale_row;
-  to_pieces<PieceCount<T>::N>(f, [&](int q, uint2 codes, uint32_t s) {
-    if (!live) return;
-    planes[q * piece_words + u] = codes;
-    if ((word & 3) == 0) sr[q * piece_scales + (word >> 2)] = (uint8_t)s;
-    if (word + 1 == words.d)
-      for (int b = (int)words.d / 4; b < scale_row; ++b) sr[q * piece_scales + b] = 0;
-  });
+  const uint64_t seg = (uint64_t)blockIdx.x * (kSplitThreads / 32) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (seg >= segments) return;
+  const int64_t row = (int64_t)(seg / per_row);
+  const int word0 = (int)(seg - (uint64_t)row * per_row) * (32 * kSplitWords) + lane;
+  float f[kSplitWords][8];
+#pragma unroll
+  for (int i = 0; i < kSplitWords; ++i) load_x(x + row * x_stride, (word0 + 32 * i) * 8, K, vec, f[i]);
+  uint2* out = planes + row * words;
+  uint8_t* sr = scales + row * scale_row;
+  const int64_t piece_words = M * words, piece_scales = M * scale_row;
+#pragma unroll
+  for (int i = 0; i < kSplitWords; ++i) {
+    const int word = word0 + 32 * i;
+    to_pieces<PieceCount<T>::N>(f[i], [&](int q, uint2 codes, uint32_t s) {
+      if (word < words) out[q * piece_words + word] = codes;
+      if ((lane & 3) == 0 && (word >> 2) < scale_row) sr[q * piece_scales + (word >> 2)] = (uint8_t)s;       // blocks behind K: zero
+    });
+  }
+  const int end = (word0 - lane + 32 * kSplitWords) >> 2;      // the row's last segment: scale bytes behind its own blocks
+  if ((word0 - lane) + 32 * kSplitWords >= words && end + lane < scale_row)
+#pragma unroll
+    for (int q = 0; q < PieceCount<T>::N; ++q) sr[q * piece_scales + end + lane] = 0;
 }
 
 inline int mx_pieces(int dtype) { return dtype == AIQ_DTYPE_F32 ? 5 : dtype == AIQ_DTYPE_F16 ? 3 : 2; }
@@ -674,11 +685,12 @@ int x_vec(const MxProduct& p) {
 
 template <typename T>
 aiq_status_t split_x(const MxProduct& p, uint8_t* planes, uint8_t* scales, cudaStream_t s) {
-  const uint32_t words = (uint32_t)(mx_plane_row(p.K) / 8);
-  const uint64_t units = (uint64_t)p.M * words;
-  mx_split_x_kernel<T><<<(unsigned)((units + kSplitThreads - 1) / kSplitThreads), kSplitThreads, 0, s>>>(
-      static_cast<const T*>(p.x), p.x_stride, p.K, p.M, x_vec<T>(p), FastDiv(words), (int)mx_scale_row_bytes(p.K), units,
-      reinterpret_cast<uint2*>(planes), scales);
+  const int words = (int)(mx_plane_row(p.K) / 8);
+  const uint32_t per_row = (uint32_t)((words + 32 * kSplitWords - 1) / (32 * kSplitWords));
+  const uint64_t segments = (uint64_t)p.M * per_row, blocks = (segments + kSplitThreads / 32 - 1) / (kSplitThreads / 32);
+  if (blocks > 0x7FFFFFFF) return set_error(AIQ_ERR_SHAPE, "mx_split_x: M=%d K=%d", p.M, p.K);
+  mx_split_x_kernel<T><<<(unsigned)blocks, kSplitThreads, 0, s>>>(static_cast<const T*>(p.x), p.x_stride, p.K, p.M, x_vec<T>(p), segments, per_row, words,
+                                                                (int)mx_scale_row_bytes(p.K), reinterpret_cast<uint2*>(planes), scales);
   AIQ_LAUNCH_CHECK("mx_split_x");
   return AIQ_OK;
 }
