@@ -100,6 +100,9 @@ def test_every_code_and_scale():
 
 SHAPES = [(1, 1, 1), (3, 33, 2), (8, 32, 1), (10, 64, 1), (129, 100, 5), (64, 320, 9), (200, 609, 17), (128, 512, 33), (1280, 320, 1),
           (1000, 1281, 4), (257, 2500, 130), (512, 1024, 300), (384, 4097, 64), (130, 8192, 3),
+          # beyond the kernel for few rows: split K ranges, rows of x beside and above each other, odd ends everywhere
+          (129, 4100, 17), (200, 6000, 33), (1001, 1300, 20), (5671, 609, 37), (130, 9000, 70), (1000, 3001, 48), (64, 20000, 9), (3, 70000, 40),
+          (260, 3100, 129), (700, 640, 257), (128, 512, 600),
           # long K ranges per block, more tiles than SMs
           (9500, 2176, 5), (9500, 2176, 16), (19000, 1100, 7), (1290, 650, 3500)]
 
@@ -148,7 +151,7 @@ def test_strides_and_what_lies_around(dtype, m):
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
-@pytest.mark.parametrize("m", [1, 40])
+@pytest.mark.parametrize("m", [1, 40, 120])
 def test_values_of_every_size(dtype, m):
     """Blocks of x and of W whose sizes lie far apart, all-zero blocks and rows, weights near both ends of the scales."""
     dt, n, k = TYPES[dtype], 160, 640
@@ -174,7 +177,7 @@ def test_values_of_every_size(dtype, m):
     assert (y[:, 0] == 0).all()
 
 
-@pytest.mark.parametrize("m", [1, 24])
+@pytest.mark.parametrize("m", [1, 24, 250])
 def test_nan_scales_and_nonfinite_activations_stay_in_their_rows(m):
     dt, n, k = torch.float32, 140, 300
     w = weights(n, k, 21)
@@ -249,6 +252,51 @@ def test_captured_calls_on_two_streams(dtype):
             ez = torch.empty_like(z)
             b.aiq_mx_matmul(vc, vs, codes, scales, None, k, ez)
             assert torch.equal(y, ey) and torch.equal(z, ez)
+
+
+@pytest.mark.parametrize("m", [1, 24, 250])
+def test_nan_blocks_of_either_matrix(m):
+    """aiq_mx_matmul: a NaN block makes its row or column NaN and nothing else."""
+    b, n, k = binding(), 140, 1300
+    w, x = weights(n, k, 61), activations(m, k, torch.float32, 62)
+    w[7, 1299] = float("inf")
+    if m > 1:
+        x[m - 1, 33] = float("nan")
+    bc, bs = held(w)
+    ac, as_ = held(x)
+    y = torch.empty((m, n), device="cuda")
+    b.aiq_mx_matmul(ac, as_, bc, bs, None, k, y)
+    assert torch.isnan(y[:, 7]).all() and (m == 1 or torch.isnan(y[m - 1]).all())
+    rows, cols = [i for i in range(m) if m == 1 or i != m - 1], [i for i in range(n) if i != 7]
+    check(y[rows][:, cols], values(ac, as_, k)[rows], values(bc, bs, k)[cols], None, torch.float32, "mx")
+
+
+def test_two_calls_are_bit_equal():
+    """The same call twice, and among others on the same workspace."""
+    for n, k, m, dt in ((1000, 5000, 40, torch.float32), (4096, 2048, 20, torch.bfloat16), (300, 700, 3, torch.float16)):
+        codes, scales = held(weights(n, k, 71))
+        x = activations(m, k, dt, 72)
+        first = linear(codes, scales, None, x, torch.empty((m, n), dtype=dt, device="cuda"))
+        linear(codes, scales, None, activations(m, k, dt, 73), torch.empty((m, n), dtype=dt, device="cuda"))
+        assert torch.equal(first, linear(codes, scales, None, x, torch.empty((m, n), dtype=dt, device="cuda")))
+
+
+def test_scale_bytes_at_both_ends():
+    """Stored weights whose scales the quantizer seldom or never writes: 2^-127, 2^126 and 2^127."""
+    b, n, k, m = binding(), 256, 2048, 40
+    codes, scales = held(weights(n, k, 81))
+    scales[0] = 0
+    scales[1] = 254
+    scales[2] = 253
+    scales[3, ::2] = 0
+    scales[:, 64:] = 0                                       # behind the last block
+    x = activations(m, k, torch.float32, 82)
+    x[0] *= 2.0 ** -100
+    y = linear(codes, scales, None, x, torch.empty((m, n), device="cuda"))
+    w = values(codes, scales, k)
+    keep = [i for i in range(n) if i not in (1, 2)]
+    check(y[:, keep], x.double().cpu().numpy(), w[keep], None, torch.float32, "f32")
+    check(y[:1], x[:1].double().cpu().numpy(), w, None, torch.float32, "f32")
 
 
 def test_refusals_on_the_device():
