@@ -251,6 +251,12 @@ def aiq_qlinear(packed, scales, bias, N, K, bits, x, y, workspace=None, stream=N
 
 # ------------------------------------------------------------------- microscaled 4 bits
 DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
+
+# These calls take their arguments through a CPython module (csrc/mxcall.c) where it is built, else through ctypes.
+try:
+    from . import _mxcall
+except ImportError:
+    _mxcall = lib
 _dtypes = None
 
 
@@ -362,7 +368,7 @@ def aiq_mx_quantize(x, codes_out, scales_out, stream=None):
     dtype, rows, k, stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_values, codes_out, scales_out, x)
     d = x.get_device()
     s = _mx_stream(stream, d, d == codes_out.get_device() == scales_out.get_device())
-    status = lib.aiq_mx_quantize(x.data_ptr(), dtype, rows, k, stride, codes_out.data_ptr(), scales_out.data_ptr(), s)
+    status = _mxcall.aiq_mx_quantize(x.data_ptr(), dtype, rows, k, stride, codes_out.data_ptr(), scales_out.data_ptr(), s)
     if status:
         _check(status)
 
@@ -373,7 +379,7 @@ def aiq_mx_dequantize(codes, scales, y, stream=None):
     dtype, rows, k, stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_values, codes, scales, y)
     d = y.get_device()
     s = _mx_stream(stream, d, d == codes.get_device() == scales.get_device())
-    status = lib.aiq_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, dtype, y.data_ptr(), stride, s)
+    status = _mxcall.aiq_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, k, dtype, y.data_ptr(), stride, s)
     if status:
         _check(status)
 
@@ -391,7 +397,7 @@ def aiq_mx_linear(codes, scales, bias, x, y, workspace=None, stream=None):
     s = _mx_stream(stream, d, d == y.get_device() == codes.get_device() == scales.get_device()
                    and (bias is None or bias.get_device() == d) and (workspace is None or workspace.get_device() == d))
     ws, size = (_dev(workspace), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
-    status = lib.aiq_mx_linear(codes.data_ptr(), scales.data_ptr(), bias.data_ptr() if bias is not None else None, n, k, x.data_ptr(), dtype,
+    status = _mxcall.aiq_mx_linear(codes.data_ptr(), scales.data_ptr(), bias.data_ptr() if bias is not None else None, n, k, x.data_ptr(), dtype,
                                m, x_stride, y.data_ptr(), y_stride, ws, size, s)
     if status:
         _check(status)
@@ -406,7 +412,7 @@ def aiq_mx_matmul(a_codes, a_scales, b_codes, b_scales, bias, K, y, stream=None)
     d = y.get_device()
     s = _mx_stream(stream, d, d == a_codes.get_device() == a_scales.get_device() == b_codes.get_device() == b_scales.get_device()
                    and (bias is None or bias.get_device() == d))
-    status = lib.aiq_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), m, b_codes.data_ptr(), b_scales.data_ptr(), n,
+    status = _mxcall.aiq_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), m, b_codes.data_ptr(), b_scales.data_ptr(), n,
                                bias.data_ptr() if bias is not None else None, int(K), y.data_ptr(), dtype, y_stride, s)
     if status:
         _check(status)

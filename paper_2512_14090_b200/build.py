@@ -3,6 +3,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
@@ -10,6 +11,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 ROOT = os.path.dirname(PKG_DIR)
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libaiq.so")
+CALL_SRC = os.path.join(CSRC, "mxcall.c")
+CALL_PATH = os.path.join(PKG_DIR, "_mxcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
@@ -33,12 +36,28 @@ def _stale(target, deps):
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_call(force=False):
+    """The CPython entry to the microscaled calls, against libaiq.so beside it.  Where there is no C compiler or no Python header the
+    binding goes through ctypes."""
+    include = sysconfig.get_paths()["include"]
+    cc = shutil.which("gcc") or shutil.which("cc")
+    if cc is None or not os.path.exists(os.path.join(include, "Python.h")):
+        return None
+    if force or _stale(CALL_PATH, [CALL_SRC, os.path.join(ROOT, "include", "aiq.h")]):
+        cmd = [cc, "-O2", "-shared", "-fPIC", "-I", include, CALL_SRC, "-o", CALL_PATH, "-L", PKG_DIR, "-l:libaiq.so", "-Wl,-rpath,$ORIGIN"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"compiling {CALL_SRC} failed:\n{r.stdout}\n{r.stderr}")
+    return CALL_PATH
+
+
 def build(force=False, verbose=False):
-    """Compile every .cu under csrc/ and link libaiq.so.  Returns the library path."""
+    """Compile every .cu under csrc/, link libaiq.so and compile its CPython entry.  Returns the library path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))]
     headers.append(os.path.join(ROOT, "include", "aiq.h"))
     if not force and not _stale(LIB_PATH, sources() + headers):
+        build_call()
         return LIB_PATH
     nvcc = _nvcc()
     objs, todo = [], []
@@ -66,6 +85,7 @@ def build(force=False, verbose=False):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    build_call(force)
     return LIB_PATH
 
 
