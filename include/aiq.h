@@ -169,8 +169,8 @@ aiq_status_t aiq_qlinear(const void* packed, const float* scales, const float* b
  * block; 16-byte aligned.  All bytes and nibbles behind the last value or block are zero; the products rely on it.
  *
  * dtype: type of the values, AIQ_DTYPE_F32, _F16 (IEEE half) or _BF16.  x_stride, y_stride: elements from one row to the
- * next (ignored for a single row).  Rows of x may start anywhere, overlap or repeat; rows of y may not overlap.  Sizes are
- * at least 1.  All calls are asynchronous on `stream` and may be captured into a graph.
+ * next (ignored for a single row).  Rows of x may start anywhere, overlap or repeat; rows of y may not overlap
+ * one another or an input.  Sizes are 1 to 2^30.  All calls are asynchronous on `stream` and may be captured into a graph.
  */
 enum { AIQ_DTYPE_F32 = 0, AIQ_DTYPE_F16 = 1, AIQ_DTYPE_BF16 = 2 };
 size_t aiq_mx_row_bytes(int K);         /* 0 for K <= 0 */

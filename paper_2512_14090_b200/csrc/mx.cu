@@ -458,10 +458,12 @@ aiq_status_t launch_mx_product_rows(const MxProduct& p, cudaStream_t s) {
 // ---------------------------------------------------------------------------------------
 using aiq::set_error;
 
+static const int kMxMost = 1 << 30;          // of any size: what rounds a size up stays an int
+
 // AIQ_OK, or what is wrong with the sizes and pointers that every entry point takes
 static aiq_status_t mx_check(const char* what, const void* codes, const void* scales, int rows, int K) {
   if (!codes || !scales) return set_error(AIQ_ERR_INVALID_ARG, "%s: null pointer", what);
-  if (rows <= 0 || K <= 0) return set_error(AIQ_ERR_INVALID_ARG, "%s: %d rows of K=%d", what, rows, K);
+  if (rows <= 0 || K <= 0 || rows > kMxMost || K > kMxMost) return set_error(AIQ_ERR_INVALID_ARG, "%s: %d rows of K=%d", what, rows, K);
   if (((uintptr_t)codes) & 31) return set_error(AIQ_ERR_INVALID_ARG, "%s: codes not 32-byte aligned", what);
   if (((uintptr_t)scales) & 15) return set_error(AIQ_ERR_INVALID_ARG, "%s: scales not 16-byte aligned", what);
   return AIQ_OK;
@@ -513,7 +515,7 @@ extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales,
 static bool mx_rows_pay(int N, int K, int M, int log2_most) { return (double)N * K * M <= (double)(1ll << log2_most); }
 
 extern "C" size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype) {
-  if (N <= 0 || K <= 0 || M <= 0 || !aiq::mx_dtype_ok(dtype)) return 0;
+  if (N <= 0 || K <= 0 || M <= 0 || N > kMxMost || K > kMxMost || M > kMxMost || !aiq::mx_dtype_ok(dtype)) return 0;
   return mx_rows_pay(N, K, M, M <= 4 ? 24 : K % 8 == 0 ? 23 : 22) ? 0 : aiq::mx_tc_workspace_bytes(K, M, dtype);
 }
 
@@ -521,7 +523,7 @@ extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, con
                                       int M, int64_t x_stride, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,
                                       void* stream) {
   if (aiq_status_t st = mx_check("aiq_mx_linear", codes, scales, N, K)) return st;
-  if (M <= 0) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear: M=%d", M);
+  if (M <= 0 || M > kMxMost) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear: M=%d", M);
   if (aiq_status_t st = mx_check_rows("aiq_mx_linear", x, dtype, x_stride)) return st;
   if (aiq_status_t st = mx_check_out("aiq_mx_linear", y, dtype, M, N, y_stride)) return st;
   if (aiq_status_t st = mx_check_bias("aiq_mx_linear", bias)) return st;

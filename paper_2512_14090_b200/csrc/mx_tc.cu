@@ -817,8 +817,13 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
                     (double)(g.N + (KIND == 0 ? g.M : 0)) * (w_row + s_row) + sizeof(T) * (double)g.M * (g.N + (KIND == 1 ? g.K : 0)));
   if (KIND == 1)
     if (aiq_status_t st = split_x<T>(g, workspace, workspace + (size_t)p.pieces * M * mx_plane_row(g.K), s)) return st;
-  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T>, dim3(p.cluster > 1 || p.tiles < props.n_sms ? p.tiles * p.cluster : props.n_sms), dim3(kMxTcThreads),
-                                      (size_t)mx_smem_bytes(p), s, a_map, b_map, sa_map, sb_map, p, g.bias, static_cast<T*>(g.y), g.y_stride));
+  // The CTAs of a cluster wait for one another, and each waits for tensor memory, for as long as another CTA on its SM holds it.  If that
+  // one belonged to a cluster of another stream with a CTA in the same position elsewhere, neither would ever go on.  So a CTA of a
+  // cluster has its SM to itself: it asks for all of the shared memory.
+  const size_t smem = p.cluster > 1 ? (size_t)props.smem_optin : (size_t)mx_smem_bytes(p);
+  const int grid = p.cluster > 1 || p.tiles < n_sms ? p.tiles * p.cluster : n_sms;
+  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T>, dim3(grid), dim3(kMxTcThreads), smem, s, a_map, b_map, sa_map, sb_map, p,
+                                      g.bias, static_cast<T*>(g.y), g.y_stride));
   AIQ_LAUNCH_CHECK("mx_tc");
   return AIQ_OK;
 }

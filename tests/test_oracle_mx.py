@@ -58,7 +58,7 @@ def test_refusals_of_the_c_abi(aiq):
     L, E = aiq.lib, aiq.ERR_INVALID_ARG
     f32, f16 = aiq.DTYPE_F32, aiq.DTYPE_F16
     quant = lambda x=one, dt=f32, r=4, k=32, st=32, c=one, s=one: L.aiq_mx_quantize(x, dt, r, k, st, c, s, None)
-    for bad in (dict(x=None), dict(c=None), dict(s=None), dict(dt=3), dict(dt=-1), dict(r=0), dict(k=0), dict(r=-1), dict(st=-1),
+    for bad in (dict(x=None), dict(c=None), dict(s=None), dict(dt=3), dict(dt=-1), dict(r=0), dict(k=0), dict(r=-1), dict(st=-1), dict(k=(1 << 30) + 1), dict(r=2 ** 31 - 1),
                 dict(c=odd16), dict(s=odd), dict(x=odd), dict(x=one + 2)):
         assert quant(**bad) == E, bad
         assert "aiq_mx_quantize" in aiq.last_error()
@@ -76,10 +76,12 @@ def test_refusals_of_the_c_abi(aiq):
     mat = lambda ac=one, as_=one, m=4, bc=one, bs=one, n=8, b=None, k=32, y=one, dt=f16, ys=8: \
         L.aiq_mx_matmul(ac, as_, m, bc, bs, n, b, k, y, dt, ys, None)
     for bad in (dict(ac=None), dict(as_=None), dict(bc=None), dict(bs=None), dict(y=None), dict(m=0), dict(n=0), dict(k=0), dict(dt=4),
-                dict(ys=7), dict(ac=odd16), dict(bs=odd), dict(b=odd)):
+                dict(ys=7), dict(n=2 ** 31 - 1, ys=2 ** 31), dict(ac=odd16), dict(bs=odd), dict(b=odd)):
         assert mat(**bad) == E, bad
     assert aiq.lib.aiq_mx_linear_workspace_bytes(0, 32, 1, f16) == 0
     assert aiq.lib.aiq_mx_linear_workspace_bytes(64, 32, 1, 5) == 0
+    assert aiq.lib.aiq_mx_linear_workspace_bytes(64, 2 ** 31 - 1, 64, f16) == 0
+    assert lin(m=(1 << 30) + 1) == E
 
 
 def test_refusals_of_the_binding(aiq):
