@@ -9,7 +9,8 @@
 // KIND 1 (aiq_mx_linear): x enters as a sum of eight-bit floats (1 + 4 + 3 bits) with a scale per block of 32, kind::mxf8f6f4,
 //   32 k per MMA; TMA expands the weights' codes to a byte each on the way to shared memory.  Each such piece takes the next
 //   five bits of the values (four, and the sign of what is left), so that 2 / 3 / 5 of them hold a bfloat16 / half / float
-//   exactly, unless it lies far below the largest value of its block: 2^-(12 + 5 pieces) of that one is what is lost at most.
+//   exactly, unless it lies far below the largest value of its block: 2^-(12 + 5 pieces) of that one, or 2^-137, is what is lost at
+//   most.
 //   The pieces are rows of the B operand beside each other while they fit into 256 (then each has columns of its own
 //   in the sums), or further MMAs into the same columns.
 //   A pre-pass writes them into the workspace; the product starts under programmatic dependent launch and loads weights meanwhile.
@@ -24,6 +25,14 @@
 // Many tiles: one CTA per SM takes every gridDim-th; the sums leave tensor memory within microseconds and are written while
 // the next tile's MMAs run.  Few tiles: the K range is split over the CTAs of a cluster, whose sums meet in shared memory in a
 // fixed order.
+//
+// What bounds it (on the device, whole calls).  2,048 rows, 8192 x 8192: bfloat16 207 us (tensor pipe active 79 % of the 198 us after
+// the pre-pass, under the power limit), half 354, float32 575 (tiles of 128 rows: shared memory feeds an MMA every 87 cycles instead of
+// 64); both microscaled 61 us (4.5 PFLOP/s; tensor pipe 62 %: shared memory again, 120 cycles instead of 96).  One row, 8192 x 8192,
+// 14.2 us: the weight stream takes 5.7 of them, the rest is the pre-pass, set-up and first loads (3 us) and the way out (1.5 us).  Both
+// microscaled, 4096 x 4096, 16 rows 7.2 us: set-up, the first loads and the cluster's exchange.
+// What made the difference: operands of the MMAs in uniform registers (see mbar_wait_uniform and the broadcast of the warp index),
+// scale bytes requested before the weights, code that runs once per tile kept in small loops, tiles by rounds over the SMs.
 #include "mx.cuh"
 #include "tc_ptx.cuh"
 
@@ -245,7 +254,6 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
              T* __restrict__ y, int64_t y_stride) {
   using Kd = MxKind<KIND>;
   constexpr bool PROMOTE = sizeof(T) == 4, CHAINED = KIND == 1;       // CHAINED: behind the pre-pass
-  const int vec = p.y_vec;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   // Broadcast, so that the compiler sees values that are the same in the whole warp and keeps what the tensor-core instructions take

@@ -104,7 +104,7 @@ SHAPES = [(1, 1, 1), (3, 33, 2), (8, 32, 1), (10, 64, 1), (129, 100, 5), (64, 32
           (129, 4100, 17), (200, 6000, 33), (1001, 1300, 20), (5671, 609, 37), (130, 9000, 70), (1000, 3001, 48), (64, 20000, 9), (3, 70000, 40),
           (260, 3100, 129), (700, 640, 257), (128, 512, 600),
           # long K ranges per block, more tiles than SMs
-          (9500, 2176, 5), (9500, 2176, 16), (19000, 1100, 7), (1290, 650, 3500)]
+          (9500, 2176, 5), (9500, 2176, 16), (19000, 1100, 7), (1290, 650, 3500), (2500, 520, 2200), (1152, 1030, 4700)]
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
