@@ -176,12 +176,12 @@ __device__ __forceinline__ void store8(T* p, const float* f) {         // 32 byt
   }
 }
 
-// A warp takes 256 U values of one row, a lane eight at a time.  A row of y may start anywhere: with `off` elements between a store
+// A warp takes 256 U values of one row, a lane eight at a time.  With SHIFT a row of y may start anywhere: with `off` elements between a store
 // boundary and the row's start, piece w of the row is its values 8 w - off to 8 w - off + 7, whose codes are a funnel shift of
 // words w - 1 and w; the first `off` of them belong to word w - 1 and its scale.
 // Bound by memory: 8192 x 8192 29 us to bfloat16 (170 MB, 90 % of the copy rate), 48 us to float32 (71 us in 16-byte stores 32 bytes
 // apart); 8192 x 8191 36 us to bfloat16 (51 us by a value per lane).
-template <typename T, int U>
+template <typename T, int U, bool SHIFT>
 __global__ void __launch_bounds__(kMxThreads)
 mx_dequantize_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restrict__ scales, int words, int scale_row, int K, uint32_t segments,
                      FastDiv per_row, T* __restrict__ y, int64_t y_stride) {
@@ -192,7 +192,7 @@ mx_dequantize_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restri
   const uint32_t row = per_row.div(seg);
   const int word0 = (int)(seg - row * per_row.d) * (32 * U) + lane;
   T* start = y + (int64_t)row * y_stride;
-  const int off = (int)((reinterpret_cast<uintptr_t>(start) & (WIDTH - 1)) / sizeof(T));
+  const int off = SHIFT ? (int)((reinterpret_cast<uintptr_t>(start) & (WIDTH - 1)) / sizeof(T)) : 0;
   const uint32_t* cr = codes + (int64_t)row * words;
   const uint8_t* sr = scales + (int64_t)row * scale_row;
   uint32_t raw[U], before[U], sb[U], sb_before[U];
@@ -241,7 +241,8 @@ aiq_status_t dequantize_rows(const uint8_t* codes, const uint8_t* scales, int64_
   for (int64_t r = 0; r < rows; r += step) {
     const int64_t n = min(step, rows - r), segments = n * per_row;
     LaunchScope scope(AIQ_KERNEL_QUANTIZE, s, (double)n * K, (double)n * (sizeof(T) * (double)K + row_bytes + scale_row));
-    mx_dequantize_kernel<T, U><<<(unsigned)((segments + kMxWarps - 1) / kMxWarps), kMxThreads, 0, s>>>(
+    const auto kernel = aligned ? mx_dequantize_kernel<T, U, false> : mx_dequantize_kernel<T, U, true>;
+    kernel<<<(unsigned)((segments + kMxWarps - 1) / kMxWarps), kMxThreads, 0, s>>>(
         reinterpret_cast<const uint32_t*>(codes + r * row_bytes), scales + r * scale_row, (int)words, (int)scale_row, K, (uint32_t)segments,
         FastDiv(per_row), y + r * y_stride, y_stride);
     AIQ_LAUNCH_CHECK("mx_dequantize");
