@@ -179,7 +179,7 @@ __device__ __forceinline__ void store8(T* p, const float* f) {         // 32 byt
 // A warp takes 256 U values of one row, a lane eight at a time.  With SHIFT a row of y may start anywhere: with `off` elements between a store
 // boundary and the row's start, piece w of the row is its values 8 w - off to 8 w - off + 7, whose codes are a funnel shift of
 // words w - 1 and w; the first `off` of them belong to word w - 1 and its scale.
-// Bound by memory: 8192 x 8192 29 us to bfloat16 (170 MB, 90 % of the copy rate), 48 us to float32 (71 us in 16-byte stores 32 bytes
+// Bound by memory: 8192 x 8192 28 us to bfloat16 (170 MB, 91 % of the copy rate), 48 us to float32 (71 us in 16-byte stores 32 bytes
 // apart); 8192 x 8191 36 us to bfloat16 (51 us by a value per lane).
 template <typename T, int U, bool SHIFT>
 __global__ void __launch_bounds__(kMxThreads)
@@ -249,8 +249,8 @@ aiq_status_t dequantize_rows(const uint8_t* codes, const uint8_t* scales, int64_
   }
   return AIQ_OK;
 }
-// As above.  U = 1 | 2 | 4: 8192 x 8192, bfloat16 40.6 | 31.6 | 29.1 us, float32 52.6 | 47.8 | 47.8; 2000 x 2000, float32 5.2 | 5.0 | 4.7;
-// 4099 x 1283, half 6.0 | 5.6 | 6.1; 1000 x 1281, float32 2.95 | 3.0 | 3.2
+// As above.  U = 1 | 2 | 4: 8192 x 8192, bfloat16 37.8 | 28.9 | 28.4 us, float32 52.4 | 48.2 | 48.8; 2000 x 2000, float32 5.1 | 4.5 | 4.8;
+// rows off a store boundary: 8192 x 8191, bfloat16 46.0 | 37.1 | 36.0; 4099 x 1283, half 6.2 | 5.7 | 6.2; 1000 x 1281, float32 3.0 | 3.1 | 3.3
 template <typename T>
 aiq_status_t dequantize_rows(const uint8_t* codes, const uint8_t* scales, int64_t rows, int K, T* y, int64_t y_stride, cudaStream_t s) {
   const double n = (double)rows * K;
