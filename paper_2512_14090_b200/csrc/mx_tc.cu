@@ -651,18 +651,21 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 constexpr int kSplitThreads = 256;
 constexpr int kSplitWords = 2;               // words of eight values per lane
 
-// A warp takes 512 values of one row, a lane eight at a time.  Bound by memory: 2,048 x 8192 bfloat16 17.5 us with a division for every
-// word.
+// A warp takes 512 values of one row, a lane eight at a time.  2,048 x 8192, the profiler's times behind a write of 200 MB, so with old
+// lines to write back on the way: bfloat16 18.3 us (68 MB; 18.9 with a 64-bit division for the row), half 22.7, float32 28.9.  With one word
+// per lane a small x takes 2.5 us instead of 3.2, and a large one of float32 33.8; but the product's set-up and first loads of weights cover
+// the small ones (8192 x 8192, one row 14.0 us either way; 5671 x 609, 37 rows, half 8.7 instead of 8.6).
 template <typename T>
 __global__ void __launch_bounds__(kSplitThreads)
-mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int64_t M, int vec, uint64_t segments, uint32_t per_row, int words, int scale_row,
+mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int64_t M, int vec, uint32_t segments, FastDiv per_row, int words, int scale_row,
                   uint2* __restrict__ planes, uint8_t* __restrict__ scales) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const uint64_t seg = (uint64_t)blockIdx.x * (kSplitThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t seg = blockIdx.x * (kSplitThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (seg >= segments) return;
-  const int64_t row = (int64_t)(seg / per_row);
-  const int word0 = (int)(seg - (uint64_t)row * per_row) * (32 * kSplitWords) + lane;
+  const uint32_t row_of = per_row.div(seg);
+  const int64_t row = row_of;
+  const int word0 = (int)(seg - row_of * per_row.d) * (32 * kSplitWords) + lane;
   float f[kSplitWords][8];
 #pragma unroll
   for (int i = 0; i < kSplitWords; ++i) load_x(x + row * x_stride, (word0 + 32 * i) * 8, K, vec, f[i]);
@@ -696,9 +699,10 @@ aiq_status_t split_x(const MxProduct& p, uint8_t* planes, uint8_t* scales, cudaS
   const int words = (int)(mx_plane_row(p.K) / 8);
   const uint32_t per_row = (uint32_t)((words + 32 * kSplitWords - 1) / (32 * kSplitWords));
   const uint64_t segments = (uint64_t)p.M * per_row, blocks = (segments + kSplitThreads / 32 - 1) / (kSplitThreads / 32);
-  if (blocks > 0x7FFFFFFF) return set_error(AIQ_ERR_SHAPE, "mx_split_x: M=%d K=%d", p.M, p.K);
-  mx_split_x_kernel<T><<<(unsigned)blocks, kSplitThreads, 0, s>>>(static_cast<const T*>(p.x), p.x_stride, p.K, p.M, x_vec<T>(p), segments, per_row, words,
-                                                                (int)mx_scale_row_bytes(p.K), reinterpret_cast<uint2*>(planes), scales);
+  if (segments > 0x7FFFFF00) return set_error(AIQ_ERR_SHAPE, "mx_split_x: M=%d K=%d", p.M, p.K);     // x and its pieces would be over 1.5 TB
+  mx_split_x_kernel<T><<<(unsigned)blocks, kSplitThreads, 0, s>>>(static_cast<const T*>(p.x), p.x_stride, p.K, p.M, x_vec<T>(p), (uint32_t)segments,
+                                                                   FastDiv(per_row), words, (int)mx_scale_row_bytes(p.K),
+                                                                   reinterpret_cast<uint2*>(planes), scales);
   AIQ_LAUNCH_CHECK("mx_split_x");
   return AIQ_OK;
 }
