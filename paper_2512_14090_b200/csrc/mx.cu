@@ -415,12 +415,231 @@ aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
   return product_rows<4, 2, X, T>(p, x, s);
 }
 
+// ---------------------------------------------------------------------------------------
+// the product, one row of x, in integers
+// ---------------------------------------------------------------------------------------
+// Twice an element is an integer of -12 to 12, and a block of x is P planes of bytes times a power of two, so a block's sum is 8 P
+// four-product instructions.  A lane holds one block of x in registers; the warp passes 1,024 values of R channels by it, one 16-byte
+// load per lane and channel.  The warps of a CTA share out k.
+//   codes -> bytes: a permutation takes byte (code & 7) of a table of eight, or, where bit 3 of the code is set, that byte's top bit eight
+//     times.  All table bytes have it set, so the table of 2 |element| - 64 gives 255 for negative codes, the one of -2 |element| - 64
+//     with bit 3 inverted 255 for the others, and their AND is 2 element - 64.  The sums start at 64 times the block's sum of x.
+//   x -> planes: rn(x 2^(8 P - 2 - e)) in two's complement, 2^e <= largest |x| < 2^(e + 1); top byte signed.  What is rounded off is at most
+//     2^-(8 P - 1) of the largest: three planes for bfloat16, four for half, one (its own codes) for a microscaled x.
+// Bound by instruction issue: 110 to 120 a block and lane, issue slots 65 to 75 % busy, 60 % of them in the integer pipe.  On the device,
+// float kernel or tensor cores | this one, weights from memory: bfloat16 2000 x 2000 4.7 | 3.8 us, 8192 x 1024 6.0 | 4.7,
+// 1024 x 8192 6.0 | 4.8, 4096 x 4096 9.3 | 6.5; half, 4096 x 4096 8.5 | 6.8; microscaled 2000 x 2000 4.8 | 2.9, 4096 x 4096 7.2 | 4.7.
+// Few channels leave SMs without work: 70 x 16500 5.3 | 5.9.
+// Two groups of channels on their way instead of one: 4096 x 4096 6.6 -> 6.9; 24 warps of 80 registers 6.9 instead of 6.8; default
+// caching of the codes instead of streaming 6.5 -> 6.8.
+// From here on it is faster than the float kernel: one row, half, 1280 x 320 2.7 us by that one, 2.9 by this; bfloat16, 1000 x 1281 3.1 by both.
+constexpr int64_t kOneFrom = 1 << 20;
+constexpr int kOneRow = 4;                       // channels at a time
+constexpr int kOneWarps = 16, kOneChannels = 64; // at most, per CTA
+
+// 2^(s - 127) of two scale bytes, NaN for 255
+__device__ __forceinline__ float2 mx_scale2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 s;\n\tcvt.u16.u32 s, %1;\n\tcvt.rn.bf16x2.ue8m0x2 %0, s;\n\t}" : "=r"(r) : "r"(a | b << 8));
+  return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint32_t permute(uint32_t lo, uint32_t hi, uint32_t sel) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(lo), "r"(hi), "r"(sel));
+  return r;
+}
+__device__ __forceinline__ int dot4(uint32_t a, uint32_t b, int c, bool b_signed) {
+  int r;
+  if (b_signed) asm("dp4a.s32.s32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  else asm("dp4a.s32.u32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+// eight codes as 2 element - 64, the first in the lowest byte
+__device__ __forceinline__ uint2 biased8(uint32_t c) {
+  const uint32_t n = c ^ 0x88888888u;
+  return make_uint2(permute(0xC3C2C1C0u, 0xCCC8C6C4u, c) & permute(0xBDBEBFC0u, 0xB4B8BABCu, n),
+                    permute(0xC3C2C1C0u, 0xCCC8C6C4u, c >> 16) & permute(0xBDBEBFC0u, 0xB4B8BABCu, n >> 16));
+}
+
+// a lane's block of x
+template <int P>
+struct OneBlock {
+  uint32_t plane[P][8];
+  int start[P];
+  float high, low, last;                         // the block's sum is (planes from 2 on * high + planes 0 and 1 * low) * weights' scale * last
+};
+template <int P>
+__device__ __forceinline__ void one_block_unit(OneBlock<P>& b, int e, bool dead) {
+  // the block is plane sums times 2^e, |e| < 200: half of it on each side of the weights' scale, behind a common 2^-32, so that nothing
+  // overflows or loses bits on the way that would not in the result
+  const int a = (e + 32) >> 1, z = e + 32 - a;
+  b.low = __uint_as_float((uint32_t)(a - 32 + 127) << 23);
+  b.high = __uint_as_float((uint32_t)(a - 16 + 127) << 23);
+  b.last = dead ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(z + 127) << 23);
+#pragma unroll
+  for (int q = 0; q < P; ++q) {
+    int s = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s = dot4(0x01010101u, b.plane[q][w], s, q == P - 1);
+    b.start[q] = 64 * s;
+  }
+}
+
+template <typename T>
+struct OneOf {                                   // x in 16 bits
+  static constexpr int P = std::is_same<T, __half>::value ? 4 : 3;
+  const T* x;
+  bool vec;
+  __device__ __forceinline__ void get(OneBlock<P>& b, int k, int K) const {
+    float f[32];
+    if (vec && k + 32 <= K) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load8(x + k + 8 * i, f + 8 * i);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) f[j] = k + j < K ? to_float(x[k + j]) : 0.f;
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+    const bool dead = top >= 0x7F800000u;
+    // a power of two in two factors, both in range
+    const int e = max((int)(top >> 23) - 127, -126), up = dead ? 0 : 8 * P - 2 - e, half = up >> 1;
+    const float u0 = __uint_as_float((uint32_t)(half + 127) << 23), u1 = __uint_as_float((uint32_t)(up - half + 127) << 23);
+    int v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = dead ? 0 : __float2int_rn(f[j] * u0 * u1);
+#pragma unroll
+    for (int w = 0; w < 8; ++w)
+#pragma unroll
+      for (int q = 0; q < P; ++q) {
+        const uint32_t sel = q | (4 + q) << 4;
+        b.plane[q][w] = permute(permute(v[4 * w], v[4 * w + 1], sel), permute(v[4 * w + 2], v[4 * w + 3], sel), 0x5410);
+      }
+    one_block_unit(b, -up - 1, dead);
+  }
+};
+struct OneHeld {                                 // x microscaled
+  static constexpr int P = 1;
+  const uint8_t *codes, *scales;
+  __device__ __forceinline__ void get(OneBlock<1>& b, int k, int K) const {
+    uint4 c = make_uint4(0, 0, 0, 0);
+    uint32_t s = 127;
+    if (k < K) {
+      c = *reinterpret_cast<const uint4*>(codes + (k >> 1));
+      s = scales[k >> 5];
+    }
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint2 u = biased8(w[i]);
+      b.plane[0][2 * i] = __vadd4(u.x, 0x40404040u);
+      b.plane[0][2 * i + 1] = __vadd4(u.y, 0x40404040u);
+    }
+    one_block_unit(b, s == 255 ? 0 : (int)s - 127 - 2, s == 255);
+  }
+};
+
+template <typename X, typename T>
+__global__ void __launch_bounds__(32 * kOneWarps, X::P == 1 ? 2 : 1)
+mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t row_bytes, int64_t scale_row,
+                      const float* __restrict__ bias, int N, int K, int channels, T* __restrict__ y) {
+  constexpr int R = kOneRow, P = X::P;
+  __shared__ float part[kOneChannels * kOneWarps];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int n0 = blockIdx.x * channels, n_end = min(N - n0, channels);
+  const int blocks = (int)(row_bytes >> 4);
+  for (int b0 = warp * 32; b0 < blocks; b0 += warps * 32) {
+    const int block = b0 + lane;
+    // behind a row's end a lane reads the row's last block, and has zeros for x
+    const uint32_t at = (uint32_t)min(block, blocks - 1), at16 = at * 16;
+    uint4 next[R];
+    uint32_t next_s[R];
+    auto load = [&](int n) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int64_t row = min(n0 + n + i, N - 1);
+        next[i] = __ldcs(reinterpret_cast<const uint4*>(codes + row * row_bytes + at16));
+        next_s[i] = *(scales + row * scale_row + at);
+      }
+    };
+    load(0);
+    OneBlock<P> xb;
+    x.get(xb, min(block, 0x3FFFFFF) * 32, K);
+    for (int n = 0; n < n_end; n += R) {
+      uint4 c[R];
+      float ws[R], v[R];
+#pragma unroll
+      for (int i = 0; i < R; i += 2) {
+        const float2 two = mx_scale2(next_s[i], next_s[i + 1]);
+        ws[i] = two.x; ws[i + 1] = two.y;
+        c[i] = next[i]; c[i + 1] = next[i + 1];
+      }
+      if (n + R < n_end) load(n + R);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        int s[P];
+#pragma unroll
+        for (int q = 0; q < P; ++q) s[q] = xb.start[q];
+        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint2 u = biased8(w[j]);
+#pragma unroll
+          for (int q = 0; q < P; ++q) s[q] = dot4(u.y, xb.plane[q][2 * j + 1], dot4(u.x, xb.plane[q][2 * j], s[q], q == P - 1), q == P - 1);
+        }
+        float sum;
+        if constexpr (P == 1) sum = (float)s[0] * xb.low;
+        else if constexpr (P == 3) sum = fmaf((float)s[2], xb.high, (float)(s[1] * 256 + s[0]) * xb.low);
+        else sum = fmaf((float)(s[3] * 256 + s[2]), xb.high, (float)(s[1] * 256 + s[0]) * xb.low);
+        v[i] = sum * ws[i] * xb.last;
+      }
+      // the warp's sums of four channels at once: lanes 0, 8, 16 and 24 end up with one each
+      const bool up = lane & 16, odd = lane & 8;
+      const float a0 = (up ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[2], 16);
+      const float a1 = (up ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, up ? v[1] : v[3], 16);
+      float a = (odd ? a1 : a0) + __shfl_xor_sync(0xffffffffu, odd ? a0 : a1, 8);
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+      if ((lane & 7) == 0) {
+        float* to = part + (n + (lane >> 3)) * warps + warp;
+        *to = b0 == warp * 32 ? a : *to + a;
+      }
+    }
+  }
+  __syncthreads();
+  for (int n = threadIdx.x; n < n_end; n += blockDim.x) {
+    float v = 0.f;
+    for (int w = 0; w < warps; ++w) v += part[n * warps + w];
+    y[n0 + n] = from_float<T>(v + (bias ? bias[n0 + n] : 0.f));
+  }
+}
+
+template <typename X, typename T>
+aiq_status_t product_row(const MxProduct& p, X x, cudaStream_t s) {
+  DeviceProps props;
+  if (aiq_status_t st = current_device_props(&props)) return st;
+  const int64_t row_bytes = mx_row_bytes(p.K), scale_row = mx_scale_row_bytes(p.K);
+  const int64_t slices = (row_bytes / 16 + 31) / 32;
+  const int warps = (int)min(slices, (int64_t)kOneWarps), ctas = props.n_sms * ((X::P == 1 ? 32 : 16) / warps);   // as many warps as an SM holds
+  const int channels = min(kOneChannels, ((p.N + ctas - 1) / ctas + kOneRow - 1) / kOneRow * kOneRow);
+  LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * p.N * p.K,
+                    (double)(p.N + (p.x ? 0 : 1)) * (row_bytes + scale_row) + sizeof(T) * (double)(p.N + (p.x ? p.K : 0)));
+  mx_product_row_kernel<X, T><<<(p.N + channels - 1) / channels, 32 * warps, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N, p.K,
+                                                                                    channels, static_cast<T*>(p.y));
+  AIQ_LAUNCH_CHECK("mx_product_row");
+  return AIQ_OK;
+}
+
 template <typename T>
 aiq_status_t product_rows(const MxProduct& p, cudaStream_t s) {
   if (p.x) {
     const bool vec = (((uintptr_t)p.x) & 15) == 0 && (p.M == 1 || p.x_stride * (int64_t)sizeof(T) % 16 == 0);
+    if constexpr (sizeof(T) == 2)
+      if (p.M == 1 && (int64_t)p.N * p.K > kOneFrom) return product_row<OneOf<T>, T>(p, OneOf<T>{static_cast<const T*>(p.x), vec}, s);
     return product_rows<RowsOf<T>, T>(p, RowsOf<T>{static_cast<const T*>(p.x), p.x_stride, vec}, s);
   }
+  if (p.M == 1) return product_row<OneHeld, T>(p, OneHeld{p.x_codes, p.x_scales}, s);
   return product_rows<RowsHeld, T>(p, RowsHeld{p.x_codes, p.x_scales, mx_row_bytes(p.K), mx_scale_row_bytes(p.K)}, s);
 }
 
@@ -509,15 +728,16 @@ extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales,
 
 // Whether the kernel for few rows and small matrices beats the tensor-core kernel, whose time below 2^22 products is its chain of
 // set-up, first loads and last stores.  On the device, rows | tensor cores (linear layer: with its pre-pass, a second launch):
-//   linear, bf16     1 row: 1280 x 320 2.6 | 7.0 us, 2000 x 2000 4.7 | 8.2, 4096 x 4096 9.2 | 9.7, 8192 x 8192 28 | 15.5
+//   linear, bf16     1 row (integers from 2^20 on): 1280 x 320 2.6 | 7.0 us, 2000 x 2000 3.8 | 8.2, 4096 x 4096 6.5 | 9.7, 8192 x 4096 9.5 | 10.8, 8192 x 8192 14.6 | 14.4,
+//                    28000 x 8192 43 | 34;  float32 4096 x 4096 9.2 | 9.7, 8192 x 8192 28 | 15.5
 //                    4 rows: 724 x 724 4.9 | 7.5, 2000 x 2000 8.4 | 8.2;  8 rows, 724 x 724 5.6 | 6.9, 720 x 720 4.3 | 7.0;
 //                    16 rows, 724 x 724 (rows that do not start on 16 bytes) 9.4 | 7.0, 720 x 720 5.4 | 7.0, 300 x 2000 6.9 | 7.2
-//   both microscaled 1 row: 2000 x 2000 4.8 | 6.3, 4096 x 4096 10.0 | 7.6;  8 rows, 300 x 300 3.2 | 4.9;  4 rows, 2000 x 2000 8.0 | 6.4
+//   both microscaled 1 row: 2000 x 2000 2.9 | 6.3, 4096 x 4096 4.7 | 7.6, 8192 x 4096 6.8 | 10.0, 8192 x 8192 12.0 | 12.0, 28000 x 8192 29 | 26;  8 rows, 300 x 300 3.2 | 4.9;  4 rows, 2000 x 2000 8.0 | 6.4
 static bool mx_rows_pay(int N, int K, int M, int log2_most) { return (double)N * K * M <= (double)(1ll << log2_most); }
 
 extern "C" size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype) {
   if (N <= 0 || K <= 0 || M <= 0 || N > kMxMost || K > kMxMost || M > kMxMost || !aiq::mx_dtype_ok(dtype)) return 0;
-  return mx_rows_pay(N, K, M, M <= 4 ? 24 : K % 8 == 0 ? 23 : 22) ? 0 : aiq::mx_tc_workspace_bytes(K, M, dtype);
+  return mx_rows_pay(N, K, M, M == 1 && dtype != AIQ_DTYPE_F32 ? 25 : M <= 4 ? 24 : K % 8 == 0 ? 23 : 22) ? 0 : aiq::mx_tc_workspace_bytes(K, M, dtype);
 }
 
 extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
@@ -559,6 +779,6 @@ extern "C" aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales,
   p.x_scales = static_cast<const uint8_t*>(a_scales);
   p.y = y; p.y_stride = y_stride;
   p.N = N; p.K = K; p.M = M; p.dtype = dtype;
-  if (mx_rows_pay(N, K, M, M == 1 ? 23 : 22)) return aiq::launch_mx_product_rows(p, (cudaStream_t)stream);
+  if (mx_rows_pay(N, K, M, M == 1 ? 25 : 22)) return aiq::launch_mx_product_rows(p, (cudaStream_t)stream);
   return aiq::launch_mx_product_tc(p, nullptr, (cudaStream_t)stream);
 }

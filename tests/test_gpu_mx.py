@@ -315,3 +315,109 @@ def test_refusals_on_the_device():
     assert e.value.status == b.ERR_WORKSPACE_TOO_SMALL
     with pytest.raises(b.AiqError):                          # rows of y on top of each other
         b.aiq_mx_linear(codes, scales, None, x, y[:1].expand(64, 256))
+
+
+# One row of x against more than 2^20 weights: a kernel of its own, which multiplies integers.  Its x is held closer than the pieces that
+# the bound counts (2^-23 of a block's largest for bfloat16, 2^-31 for half, against 2^-22 and 2^-27).  Additions: one within a block, 5
+# in a warp, at most 15 over warps and K / 16384 over rounds, fewer than the bound's K / 32 + 64.  A block's planes are joined from
+# sums of up to 2^25 units of at most 2^-22 of its largest |x|, rounded to 24 bits: one unit of 2^-22 2^-6 at bfloat16, far less at half.
+ONE_ROW = [(1100, 1000), (4099, 257), (9000, 120), (70, 16500), (33, 33000), (1031, 2049), (40000, 32), (131073, 8), (1025, 1024), (4097, 4096),
+           (8200, 4100)]
+
+
+def _one_row(kind, codes, scales, bias, x, k, workspace=True):
+    n = codes.shape[0]
+    if kind == "mx":
+        y = torch.full((1, n), float("nan"), device="cuda")
+        binding().aiq_mx_matmul(*x, codes, scales, bias, k, y)
+        return y
+    return linear(codes, scales, bias, x, torch.full((1, n), float("nan"), dtype=TYPES[kind], device="cuda"), workspace)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "mx"])
+@pytest.mark.parametrize("n,k", ONE_ROW)
+def test_one_row(kind, n, k):
+    dt = TYPES.get(kind, torch.float32)
+    codes, scales = held(weights(n, k, n + k))
+    w = values(codes, scales, k)
+    bias = torch.randn(n, generator=torch.Generator().manual_seed(3)).cuda() if n % 2 else None
+    for skip in (0, 1) if kind != "mx" else (0,):
+        x = activations(1, k + skip, dt, k)[:, skip:]
+        given = held(x) if kind == "mx" else x
+        xv = values(*given, k) if kind == "mx" else x.double().cpu().numpy()
+        for workspace in (True, False) if n * k > 2 ** 25 else (True,):
+            y = _one_row(kind, codes, scales, bias, given, k, workspace)
+            check(y, xv, w, bias.cpu().numpy() if bias is not None else None, dt, kind, f"skip {skip} workspace {workspace}")
+            assert torch.equal(y, _one_row(kind, codes, scales, bias, given, k, workspace))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "mx"])
+def test_one_row_of_every_size(kind):
+    """Blocks of x from the type's subnormal values to 2^100, weights' scales that bring them back, zeros, negative and mixed signs."""
+    dt, n, k = TYPES.get(kind, torch.float32), 2050, 640
+    w = weights(n, k, 91).cpu()
+    w[3, 40:80] = 0
+    codes, scales = held(w.cuda())
+    x = activations(1, k, torch.float32, 92).cpu()
+    x[0, 64:96] = 0
+    x[0, 96:128] = -x[0, 96:128].abs()
+    x[0, 128:160] *= torch.logspace(-8, 0, 32)                     # far below the block's largest
+    if kind == "f16":
+        x[0, :32] *= 2.0 ** -16
+        x[0, 32:64] = 60000.0
+        scales[:, 0] = 140
+        scales[:, 1] = 100
+    else:
+        x[0, :32] *= 2.0 ** -122
+        x[0, 32:64] *= 2.0 ** 100
+        x[0, 160:192] = torch.arange(1, 33) * 2.0 ** -133
+        scales[:, 0] = 245
+        scales[:, 1] = 10
+        scales[:, 5] = 254
+    x = x.to(dt).cuda()
+    given = held(x) if kind == "mx" else x
+    xv = values(*given, k) if kind == "mx" else x.double().cpu().numpy()
+    check(_one_row(kind, codes, scales, None, given, k), xv, values(codes, scales, k), None, dt, kind)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "mx"])
+def test_one_row_with_nan_and_infinity(kind):
+    dt, n, k = TYPES.get(kind, torch.float32), 1030, 1100
+    w = weights(n, k, 93)
+    w[5, 1099] = float("nan")
+    w[1029, 0] = float("inf")
+    codes, scales = held(w)
+    for what in (None, float("nan"), float("inf"), -float("inf")):
+        x = activations(1, k, dt, 94)
+        if what is not None:
+            x[0, 1070] = what
+        given = held(x) if kind == "mx" else x
+        y = _one_row(kind, codes, scales, None, given, k)
+        if what is not None:
+            assert torch.isnan(y).all()
+            continue
+        assert torch.isnan(y[0, [5, 1029]]).all()
+        keep = [i for i in range(n) if i not in (5, 1029)]
+        xv = values(*given, k) if kind == "mx" else x.double().cpu().numpy()
+        check(y[:, keep], xv, values(codes, scales, k)[keep], None, dt, kind)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_one_row_captured_and_what_lies_around(kind):
+    """A captured call reads the x of its replay; elements of y's buffer beside the row stay as they were."""
+    dt, n, k = TYPES[kind], 2051, 520
+    codes, scales = held(weights(n, k, 95))
+    w = values(codes, scales, k)
+    x, wide = activations(1, k, dt, 96), torch.full((1, n + 7), 7.0, dtype=dt, device="cuda")
+    y = wide[:, 3:3 + n]
+    linear(codes, scales, None, x, y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        linear(codes, scales, None, x, y)
+    for seed in (97, 98):
+        x.copy_(activations(1, k, dt, seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        check(y, x.double().cpu().numpy(), w, None, dt, kind)
+        assert (wide[:, :3] == 7.0).all() and (wide[:, 3 + n:] == 7.0).all()
