@@ -182,7 +182,8 @@ size_t aiq_mx_scale_row_bytes(int K);   /* 0 for K <= 0 */
  * and zero codes.  Deterministic; the padding is written too. */
 aiq_status_t aiq_mx_quantize(const void* x, int dtype, int rows, int K, int64_t x_stride, void* codes_out,
                              void* scales_out, void* stream);
-/* codes and scales -> y: the values above, rounded to nearest even in `dtype` (exact in float32, and in bfloat16). */
+/* codes and scales -> y: the values above, rounded to nearest even in `dtype`: exact in float32 and in bfloat16, save that what lies
+ * above their range (elements of 4 and 6 under s = 253, of 2 to 6 under 254; the quantizer writes at most 252) becomes infinity. */
 aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales, int rows, int K, int dtype, void* y,
                                int64_t y_stride, void* stream);
 

@@ -265,11 +265,18 @@ aiq_status_t dequantize_rows(const uint8_t* codes, const uint8_t* scales, int64_
 // A warp computes R output channels for MT rows of x, or a share of their k.  A lane takes a word of eight codes at a time, so that
 // the loads of a warp are whole lines: 128 bytes of codes, and the 256 values of x that belong to them.  All loads of U words are
 // under way before the first is used.  float32 throughout, two products per instruction.
+// An element times its scale reaches 6 * 2^127, which no float32 holds.  So a quarter of it is multiplied, exact at both ends (from
+// 1.5 * 2^127 to 2^-130), and the sum is scaled back at the end: a sum that overflows would do so without it, too.  Below 2^-124 (2^-122 with two
+// microscaled matrices) a sum has fewer than 24 bits.
 constexpr int kRowChannels = 2;
+__device__ __forceinline__ float mx_quarter_scale(uint32_t s) {        // 2^(s - 129); NaN for 255
+  return __uint_as_float(s < 3 ? 0x00100000u << s : s == 255 ? 0x7FC00000u : (s - 2) << 23);
+}
 
 // eight values of x from k on (k a multiple of 8), as they are loaded and as floats; zero behind K
 template <typename T>
 struct RowsOf {
+  static constexpr float UNIT = 1.f;               // of values()
   struct Raw { uint4 v[sizeof(T) / 2]; };
   const T* x;
   int64_t stride;
@@ -297,6 +304,7 @@ struct RowsOf {
   }
 };
 struct RowsHeld {
+  static constexpr float UNIT = 4.f;
   struct Raw { uint32_t codes, scale; };
   const uint8_t *codes, *scales;
   int64_t row_bytes, scale_row;
@@ -306,7 +314,7 @@ struct RowsHeld {
   static __device__ __forceinline__ Raw none() { return Raw{0u, 0u}; }
   static __device__ __forceinline__ void values(const Raw& r, float* f) {
     mx_expand8(r.codes, f);
-    const float s = mx_scale(r.scale);
+    const float s = mx_quarter_scale(r.scale);
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] *= s;
   }
@@ -352,7 +360,7 @@ mx_product_rows_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __
         for (int i = 0; i < R; ++i) {
           float f[8];
           mx_expand8(raw[i][u], f);
-          const float s = mx_scale(sb[i][u]);
+          const float s = mx_quarter_scale(sb[i][u]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) wf[i][j] = mul2(pack2(f[2 * j], f[2 * j + 1]), pack2(s, s));
         }
@@ -384,7 +392,7 @@ mx_product_rows_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __
       const int i = lane / MT, r = lane % MT;
       float v = 0.f;
       for (int k = 0; k < k_warps; ++k) v += part[warp + k][lane];
-      if (n0 + i < N && m0 + r < M) y[(m0 + r) * y_stride + n0 + i] = from_float<T>(v + (bias ? bias[n0 + i] : 0.f));
+      if (n0 + i < N && m0 + r < M) y[(m0 + r) * y_stride + n0 + i] = from_float<T>(v * (4.f * X::UNIT) + (bias ? bias[n0 + i] : 0.f));
     }
     if (k_warps > 1) __syncthreads(); else __syncwarp();
   }
