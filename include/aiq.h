@@ -188,15 +188,16 @@ aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales, int rows, 
                                int64_t y_stride, void* stream);
 
 /* The linear layer with microscaled weights:  y[m][n] = sum_k x[m][k] W[n][k] + bias[n],  W [N][K] as codes and scales,
- * x [M][K] and y [M][N] of `dtype`, bias float32 [N] or NULL.  Products are exact, sums are float32; run-to-run identical.
+ * x [M][K] and y [M][N] of `dtype`, bias float32 [N] or NULL.  Sums are float32; run-to-run identical.
  *
- * Three kernels.  One for few rows and small matrices multiplies in float32 and needs no workspace; nor does one for a single row of
- * 16-bit values (N K > 2^20), which multiplies integers: x to within 2^-23 (bfloat16) or 2^-31 (half) of the largest of its 32
- * values, so exactly what lies above 2^-15 or 2^-20 of it.  The third, for the rest, runs on
+ * Three kernels.  Two need no workspace, and every product of theirs is exact: one for few rows and small matrices multiplies in
+ * float32, one for a single row of 16-bit values (N K > 2^20) in integers, with what those leave out of x in float32.  The third, for the rest, runs on
  * the tensor cores' block-scaled MMAs (tcgen05, kind::mxf8f6f4): a pre-pass writes x into `workspace` as a sum of eight-bit
  * floats, 2 for bfloat16, 3 for half, 5 for float32, with a scale for every 32 values.  They hold x exactly, save what lies
- * below 2^-22 (bfloat16), 2^-27 (half), 2^-37 (float32) of the largest of the 32 values; in the last two a block with an infinity or
- * a NaN makes its row of y NaN.  `workspace`: device, 16-byte aligned, aiq_mx_linear_workspace_bytes(...) bytes (0 where one of the first
+ * below 2^-22 (bfloat16), 2^-27 (half), 2^-37 (float32) of the largest of the 32 values; their products are exact.  In the last two kernels a block
+ * with an infinity or a NaN makes its row of y NaN; in float32 an infinity gives what IEEE arithmetic does.  Which kernel runs depends on the
+ * sizes, so a row's last bits depend on how many rows come with it.  `workspace`: device, 16-byte aligned,
+ * aiq_mx_linear_workspace_bytes(...) bytes (0 where one of the first
  * two is chosen or an argument is out of range), not used by two calls at a time.  NULL: the first two, whatever the size.
  * Every wait inside the tensor-core kernel is bounded (about 2 s); should one run out, the tile of y becomes NaN. */
 size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype);
@@ -204,7 +205,7 @@ aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* b
                            int M, int64_t x_stride, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,
                            void* stream);
 /* The product of two microscaled matrices:  y[m][n] = sum_k A[m][k] B[n][k] + bias[n],  A [M][K] (the activations, by
- * aiq_mx_quantize), B [N][K] (the weights), y [M][N] of `dtype`.  Products are exact, sums are float32; run-to-run identical.
+ * aiq_mx_quantize), B [N][K] (the weights), y [M][N] of `dtype`.  Products are exact, sums are float32; run-to-run identical; a row's last bits depend on M.
  * kind::mxf4 on the tensor cores, which take codes and scales as they are stored; the kernels for small matrices and for a single row as above. */
 aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales, int M, const void* b_codes, const void* b_scales, int N,
                            const float* bias, int K, void* y, int dtype, int64_t y_stride, void* stream);

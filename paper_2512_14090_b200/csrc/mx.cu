@@ -432,12 +432,16 @@ aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
 //   codes -> bytes: a permutation takes byte (code & 7) of a table of eight, or, where bit 3 of the code is set, that byte's top bit eight
 //     times.  All table bytes have it set, so the table of 2 |element| - 64 gives 255 for negative codes, the one of -2 |element| - 64
 //     with bit 3 inverted 255 for the others, and their AND is 2 element - 64.  The sums start at 64 times the block's sum of x.
-//   x -> planes: rn(x 2^(8 P - 2 - e)) in two's complement, 2^e <= largest |x| < 2^(e + 1); top byte signed.  What is rounded off is at most
-//     2^-(8 P - 1) of the largest: three planes for bfloat16, four for half, one (its own codes) for a microscaled x.
+//   x -> planes: rn(x 2^(8 P - 2 - e)) in two's complement, 2^e <= largest |x| < 2^(e + 1); top byte signed.  Three planes for bfloat16, four
+//     for half, one (its own codes) for a microscaled x.  A block's sum is then an exact integer, below 2^41, and rounded once,
+//     when it becomes a float32.
+//   What the planes cannot hold, the last bits of values below 2^-15 (bfloat16) or 2^-20 (half) of the block's largest, is multiplied value
+//     by value in float32 (one_rest): in normally distributed data one value in twenty thousand or fewer.
 // Bound by instruction issue: 110 to 120 a block and lane, issue slots 65 to 75 % busy, 60 % of them in the integer pipe.  On the device,
-// float kernel or tensor cores | this one, weights from memory: bfloat16 2000 x 2000 4.7 | 3.8 us, 8192 x 1024 6.0 | 4.7,
-// 1024 x 8192 6.0 | 4.8, 4096 x 4096 9.3 | 6.5; half, 4096 x 4096 8.5 | 6.8; microscaled 2000 x 2000 4.8 | 2.9, 4096 x 4096 7.2 | 4.7.
-// Few channels leave SMs without work: 70 x 16500 5.3 | 5.9.
+// float kernel or tensor cores | this one, weights from memory: bfloat16 2000 x 2000 4.7 | 3.7 us, 8192 x 1024 6.0 | 4.7,
+// 1024 x 8192 6.0 | 4.7, 4096 x 4096 9.3 | 6.4; half, 4096 x 4096 8.5 | 6.7; microscaled 2000 x 2000 4.8 | 2.7, 4096 x 4096 7.2 | 4.8.
+// Few channels leave SMs without work: 70 x 16500 5.3 | 5.9.  Rounding what the planes cannot hold away instead took as long; finding it with
+// float32 comparisons for every value, 0.3 to 0.6 us more.
 // Two groups of channels on their way instead of one: 4096 x 4096 6.6 -> 6.9; 24 warps of 80 registers 6.9 instead of 6.8; default
 // caching of the codes instead of streaming 6.5 -> 6.8.
 // From here on it is faster than the float kernel: one row, half, 1280 x 320 2.7 us by that one, 2.9 by this; bfloat16, 1000 x 1281 3.1 by both.
@@ -474,7 +478,10 @@ template <int P>
 struct OneBlock {
   uint32_t plane[P][8];
   int start[P];
-  float high, low, last;                         // the block's sum is (planes from 2 on * high + planes 0 and 1 * low) * weights' scale * last
+  float low, last;                               // the block's sum is the planes' * low * weights' scale * last
+  int up;                                        // the planes' values are x 2^up
+  uint32_t rest;                                 // bit j: value j may not be all in the planes
+  float first;                                   // what is left of the first of them
 };
 template <int P>
 __device__ __forceinline__ void one_block_unit(OneBlock<P>& b, int e, bool dead) {
@@ -482,7 +489,6 @@ __device__ __forceinline__ void one_block_unit(OneBlock<P>& b, int e, bool dead)
   // overflows or loses bits on the way that would not in the result
   const int a = (e + 32) >> 1, z = e + 32 - a;
   b.low = __uint_as_float((uint32_t)(a - 32 + 127) << 23);
-  b.high = __uint_as_float((uint32_t)(a - 16 + 127) << 23);
   b.last = dead ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(z + 127) << 23);
 #pragma unroll
   for (int q = 0; q < P; ++q) {
@@ -499,24 +505,50 @@ struct OneOf {                                   // x in 16 bits
   const T* x;
   bool vec;
   __device__ __forceinline__ void get(OneBlock<P>& b, int k, int K) const {
-    float f[32];
+    uint32_t raw[16];                              // two values each
     if (vec && k + 32 <= K) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load8(x + k + 8 * i, f + 8 * i);
+      for (int i = 0; i < 4; ++i) {
+        const uint4 r = reinterpret_cast<const uint4*>(x + k)[i];
+        raw[4 * i] = r.x; raw[4 * i + 1] = r.y; raw[4 * i + 2] = r.z; raw[4 * i + 3] = r.w;
+      }
     } else {
+      T t[32];
 #pragma unroll
-      for (int j = 0; j < 32; ++j) f[j] = k + j < K ? to_float(x[k + j]) : 0.f;
+      for (int j = 0; j < 32; ++j) t[j] = k + j < K ? x[k + j] : from_float<T>(0.f);
+      memcpy(raw, t, sizeof(raw));
     }
-    uint32_t top = 0;
+    // The largest |value|, and the least other than zero: with the sign bit set and one taken off, read as signed numbers, zero comes last.
+    uint32_t top2 = 0, least2 = 0x7FFF7FFFu;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
+    for (int i = 0; i < 16; ++i) {
+      top2 = __vmaxu2(top2, raw[i] & 0x7FFF7FFFu);
+      least2 = __vmins2(least2, (raw[i] | 0x80008000u) - 0x00010001u);
+    }
+    const uint32_t least1 = __vmins2(least2, least2 >> 16 | least2 << 16);
+    const uint32_t top = float_bits(max(top2 >> 16, top2 & 0xFFFFu)), least = float_bits((least1 + 1) & 0x7FFFu);
     const bool dead = top >= 0x7F800000u;
-    // a power of two in two factors, both in range
-    const int e = max((int)(top >> 23) - 127, -126), up = dead ? 0 : 8 * P - 2 - e, half = up >> 1;
-    const float u0 = __uint_as_float((uint32_t)(half + 127) << 23), u1 = __uint_as_float((uint32_t)(up - half + 127) << 23);
+    const int e = max((int)(top >> 23) - 127, -126), up = dead ? 0 : 8 * P - 2 - e;
+    float f[32];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const T* h = reinterpret_cast<const T*>(&raw[i]);
+      f[2 * i] = to_float(h[0]);
+      f[2 * i + 1] = to_float(h[1]);
+    }
     int v[32];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = dead ? 0 : __float2int_rn(f[j] * u0 * u1);
+    for (int j = 0; j < 32; ++j) v[j] = dead ? 0 : integer(f[j], up);
+    b.up = up;
+    b.rest = 0;
+    // all bits of a value are in the planes where its last one is: at its exponent less 7 (bfloat16) or 10 (half)
+    const int lowest = (P == 4 ? 10 : 7) + 127 - up;               // of a float32's exponent field
+    if ((int)(least >> 23) < lowest && !dead && least != 0) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if ((__float_as_uint(f[j]) & 0x7FFFFFFFu) - 1 < ((uint32_t)lowest << 23) - 1) b.rest |= 1u << j;
+      b.first = left(to_float(x[k + __ffs(b.rest) - 1]), up);
+    }
 #pragma unroll
     for (int w = 0; w < 8; ++w)
 #pragma unroll
@@ -526,7 +558,47 @@ struct OneOf {                                   // x in 16 bits
       }
     one_block_unit(b, -up - 1, dead);
   }
+  // |value| of 16 bits as the bits of a float32
+  static __device__ __forceinline__ uint32_t float_bits(uint32_t a) {
+    if (P == 3) return a << 16;
+    return __float_as_uint(__half2float(__ushort_as_half((unsigned short)a)));
+  }
+  // f 2^up as an integer; the power of two is two factors, so that both are in range
+  static __device__ __forceinline__ int integer(float f, int up) {
+    const int half = up >> 1;
+    return __float2int_rn(f * __uint_as_float((uint32_t)(half + 127) << 23) * __uint_as_float((uint32_t)(up - half + 127) << 23));
+  }
+  // what that leaves out of f, exactly
+  static __device__ __forceinline__ float left(float f, int up) {
+    const int half = up >> 1;
+    return f - (float)integer(f, up) * __uint_as_float((uint32_t)(127 - half) << 23) * __uint_as_float((uint32_t)(127 - (up - half)) << 23);
+  }
 };
+// one of a word's eight elements, from bit `shift` on
+__device__ __forceinline__ float one_element(uint32_t word, int shift) {
+  uint32_t h;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(h) : "r"((word >> shift) & 0xFu));
+  return __half2float(__ushort_as_half((unsigned short)(h & 0xFFFFu)));
+}
+// The sum of what the planes of a lane's block leave out, times its codes of R channels.  The values, save the first, come from memory again:
+// nothing is held for them.
+template <typename T>
+__device__ __forceinline__ void one_rest(const OneOf<T>& x, const OneBlock<OneOf<T>::P>& b, int k, const uint4 (&c)[kOneRow], float (&sum)[kOneRow]) {
+#pragma unroll
+  for (int i = 0; i < kOneRow; ++i) sum[i] = 0.f;
+  float r = b.first;
+#pragma unroll 1
+  for (uint32_t m = b.rest; m;) {
+    const int at = __ffs(m) - 1;
+#pragma unroll
+    for (int i = 0; i < kOneRow; ++i) {
+      const uint32_t word = at & 16 ? (at & 8 ? c[i].w : c[i].z) : (at & 8 ? c[i].y : c[i].x);
+      sum[i] = fmaf(r, one_element(word, 4 * (at & 7)), sum[i]);
+    }
+    m &= m - 1;
+    if (m) r = OneOf<T>::left(to_float(x.x[k + __ffs(m) - 1]), b.up);
+  }
+}
 struct OneHeld {                                 // x microscaled
   static constexpr int P = 1;
   const uint8_t *codes, *scales;
@@ -573,7 +645,10 @@ mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __r
     };
     load(0);
     OneBlock<P> xb;
-    x.get(xb, min(block, 0x3FFFFFF) * 32, K);
+    const int k = min(block, 0x3FFFFFF) * 32;
+    x.get(xb, k, K);
+    bool any_rest = false;
+    if constexpr (P > 1) any_rest = __any_sync(0xffffffffu, xb.rest != 0);
     for (int n = 0; n < n_end; n += R) {
       uint4 c[R];
       float ws[R], v[R];
@@ -594,14 +669,22 @@ mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __r
         for (int j = 0; j < 4; ++j) {
           const uint2 u = biased8(w[j]);
 #pragma unroll
-          for (int q = 0; q < P; ++q) s[q] = dot4(u.y, xb.plane[q][2 * j + 1], dot4(u.x, xb.plane[q][2 * j], s[q], q == P - 1), q == P - 1);
+          for (int q = 0; q < P; ++q)
+            s[q] = dot4(u.y, xb.plane[q][2 * j + 1], dot4(u.x, xb.plane[q][2 * j], s[q], q == P - 1), q == P - 1);
         }
         float sum;
         if constexpr (P == 1) sum = (float)s[0] * xb.low;
-        else if constexpr (P == 3) sum = fmaf((float)s[2], xb.high, (float)(s[1] * 256 + s[0]) * xb.low);
-        else sum = fmaf((float)(s[3] * 256 + s[2]), xb.high, (float)(s[1] * 256 + s[0]) * xb.low);
+        else if constexpr (P == 3) sum = (float)((int64_t)s[2] * 65536 + (s[1] * 256 + s[0])) * xb.low;
+        else sum = (float)((int64_t)(s[3] * 256 + s[2]) * 65536 + (s[1] * 256 + s[0])) * xb.low;
         v[i] = sum * ws[i] * xb.last;
       }
+      if constexpr (P > 1)
+        if (any_rest) {
+          float rest[R];
+          one_rest(x, xb, k, c, rest);
+#pragma unroll
+          for (int i = 0; i < R; ++i) v[i] = fmaf(rest[i], ws[i], v[i]);
+        }
       // the warp's sums of four channels at once: lanes 0, 8, 16 and 24 end up with one each
       const bool up = lane & 16, odd = lane & 8;
       const float a0 = (up ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[2], 16);

@@ -43,3 +43,68 @@ def test_matmul_with_scale_bytes_at_both_ends(dtype, n, k, m):
     y = torch.full((m, n), float("nan"), dtype=dt, device="cuda")
     b.aiq_mx_matmul(ac, as_, bc, bs, None, k, y)
     check(y, values(ac, as_, k), values(bc, bs, k), None, dt, "mx")
+
+
+def _rows_of(codes, scales, k):
+    """float64 values of stored rows, on the GPU."""
+    return torch.from_numpy(values(codes, scales, k)).cuda()
+
+
+# One row: every product is exact, whatever else is in its block.  Additions: a block's 32 products become one float32 (one rounding, 2^-24 of
+# the block's sum), what the block's integers cannot hold is added value by value (32 at most, 32 roundings of a sum of small values, and one for
+# adding it), then 5 in a warp, at most 15 over warps, K / 16384 over rounds and one for the bias.  The kernel for few rows: K / 512 / 2 in a lane's
+# chain of pairs, 1 + 5 + 8 behind it.  64 + K / 512 roundings of 2^-24 of sum |x w| cover both, and half a step of the output type.
+def _check_exact_products(y, x, w, what):
+    x, w = x.double(), w.double()
+    ref, s = x @ w.t(), x.abs() @ w.abs().t()
+    err = (64 + x.shape[1] / 512) * 2.0 ** -24 * s
+    f = torch.finfo(y.dtype)
+    tol = err + f.eps / 2 * (ref.abs() + err) + f.smallest_normal * f.eps
+    worst = ((y.double() - ref).abs() / tol).max().item()
+    assert worst <= 1.0, f"{what}: error is {worst:.3g} of what is allowed"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,k", [(1100, 1000), (2048, 1024), (8200, 200), (70, 16500), (40, 40000)])
+@pytest.mark.parametrize("log2", [0, 10, 14, 20, 40])
+def test_one_row_with_values_far_apart_in_a_block(dtype, n, k, log2):
+    """One value of every block far above the others, and channels whose codes there are zero: what is left are products with the others."""
+    if dtype == "f16" and log2 > 20:
+        log2 = 28                                                      # half: from 2^-18 to 2^10
+    dt = TYPES[dtype]
+    codes, scales = held(weights(n, k, 5))
+    c = codes.clone()
+    g = torch.Generator().manual_seed(log2)
+    down = log2 // 2 + 4 if dtype == "f16" else 0                      # halves: around the middle of their range
+    x = torch.randn((1, k), generator=g)
+    at = torch.arange(7, k, 32)
+    c[: n // 2, (at // 2).cuda()] &= 0x0F                              # element 7 of a block is in a high nibble
+    x *= 2.0 ** -down
+    x[0, at] = torch.randn(len(at), generator=g).sign() * 2.0 ** (log2 - down) * 1.5
+    x[0, 3::32] *= 2.0 ** -6
+    x = x.to(dt).cuda()
+    assert torch.isfinite(x).all()
+    w = _rows_of(c, scales, k)
+    y = linear(c, scales, None, x, torch.full((1, n), float("nan"), dtype=dt, device="cuda"), workspace=False)
+    _check_exact_products(y, x, w, f"2^{log2}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_row_with_one_weight_per_channel(dtype):
+    """Each channel has one element other than zero, a power of two: y is that value of x times it, to the last bit."""
+    dt, n, k = TYPES[dtype], 2048, 1024
+    g = torch.Generator().manual_seed(3)
+    at = torch.randperm(k, generator=g).repeat(2)[:n]
+    e = torch.randint(0, 3, (n,), generator=g)                         # elements 1, 2, 4: codes 2, 4, 6
+    sign = torch.randint(0, 2, (n,), generator=g)
+    codes = torch.zeros((n, k), dtype=torch.uint8)
+    codes[torch.arange(n), at] = (2 * (e + 1) + 8 * sign).to(torch.uint8)
+    codes = (codes[:, 0::2] | (codes[:, 1::2] << 4)).contiguous().cuda()
+    scales = torch.full((n, 32), 125, dtype=torch.uint8, device="cuda")
+    x = torch.randn((1, k), generator=g) * torch.exp2(torch.randint(-12, 13, (1, k), generator=g).float())
+    if dtype == "bf16":
+        x *= torch.exp2(torch.randint(-30, 31, (1, k), generator=g).float())
+    x = x.to(dt)
+    want = (x[0, at].double() * 2.0 ** (e.double() - 2) * (1 - 2 * sign)).to(dt)
+    y = linear(codes, scales, None, x.cuda(), torch.full((1, n), float("nan"), dtype=dt, device="cuda"))
+    assert torch.equal(y[0].cpu(), want)
