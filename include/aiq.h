@@ -194,7 +194,9 @@ aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales, int rows, 
  * float32, one for a single row of 16-bit values (N K > 2^20) in integers, with what those leave out of x in float32.  The third, for the rest, runs on
  * the tensor cores' block-scaled MMAs (tcgen05, kind::mxf8f6f4): a pre-pass writes x into `workspace` as a sum of eight-bit
  * floats, 2 for bfloat16, 3 for half, 5 for float32, with a scale for every 32 values.  They hold x exactly, save what lies
- * below 2^-22 (bfloat16), 2^-27 (half), 2^-37 (float32) of the largest of the 32 values; their products are exact.  In the last two kernels a block
+ * below 2^-22 (bfloat16), 2^-27 (half), 2^-37 (float32) of the largest of the 32 values; their products are exact.  The MMAs cut a sum where
+ * float32 would round it, which costs a 16-bit result up to a tenth of its own rounding; sums that would lose more, and those of float32 results,
+ * are added up in float32 every 512 k.  In the last two kernels a block
  * with an infinity or a NaN makes its row of y NaN; in float32 an infinity gives what IEEE arithmetic does.  Which kernel runs depends on the
  * sizes, so a row's last bits depend on how many rows come with it.  `workspace`: device, 16-byte aligned,
  * aiq_mx_linear_workspace_bytes(...) bytes (0 where one of the first

@@ -14,8 +14,8 @@
 //   The pieces are rows of the B operand beside each other while they fit into 256 (then each has columns of its own
 //   in the sums), or further MMAs into the same columns.
 //   A pre-pass writes them into the workspace; the product starts under programmatic dependent launch and loads weights meanwhile.
-// Products are exact.  The tensor core drops what an addition has below the accumulator's last bit; with float32 results the
-// sums are therefore taken out every 512 k and added up in float32 registers (two sets of columns, used in turn).
+// Products are exact.  The tensor core drops what an addition has below the accumulator's last bit; with float32 results and over long K
+// (mx_promote) the sums are therefore taken out every 512 k and added up in float32 registers (PROMOTE: two sets of columns, used in turn).
 //
 //   warp 0     TMA: weights            warp 2   TMA: rows of x
 //   warp 1     MMA issuer              warp 3   TMA: scale bytes of both, 512 k at a time (16 bytes a row)
@@ -247,13 +247,13 @@ __device__ __forceinline__ void to_pieces(float* f, F put) {
   }
 }
 
-template <int KIND, typename T>
+template <int KIND, typename T, bool PROMOTE>
 __global__ void __launch_bounds__(kMxTcThreads, 1)
 mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ CUtensorMap sa_map,
              const __grid_constant__ CUtensorMap sb_map, const __grid_constant__ MxTcParams p, const float* __restrict__ bias,
              T* __restrict__ y, int64_t y_stride) {
   using Kd = MxKind<KIND>;
-  constexpr bool PROMOTE = sizeof(T) == 4, CHAINED = KIND == 1;       // CHAINED: behind the pre-pass
+  constexpr bool CHAINED = KIND == 1;              // behind the pre-pass
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   // Broadcast, so that the compiler sees values that are the same in the whole warp and keeps what the tensor-core instructions take
@@ -715,13 +715,24 @@ aiq_status_t encode(EncodeTiledFn enc, CUtensorMap* map, CUtensorMapDataType typ
   return r == CUDA_SUCCESS ? AIQ_OK : set_error(AIQ_ERR_CUDA, "cuTensorMapEncodeTiled (microscaled product) failed with code %d", (int)r);
 }
 
+// Whether sums leave the accumulator every 512 k.  With 16-bit results they may stay while what the additions drop is little beside the
+// result's own rounding.  All-positive sums lose 2^-27 of themselves an MMA: half, 640 channels, 2,100 rows, K = 2^20 (98,304 MMAs) 6.8e-4,
+// where half a step is 2.4e-4 or more; K = 2^17 8.4e-5.  The limits keep it under a tenth of half a step: half up to K = 32,768 (both
+// microscaled 196,608), bfloat16 up to 262,144 (1,048,576).  Above, tiles are 128 rows wide at most instead of 256: half, 640 channels, 2,100
+// rows, K = 2^20 7.4 -> 8.6 ms; 2,048 channels, 520 rows, K = 2^17 0.48 -> 0.76.
 template <int KIND, typename T>
+bool mx_promote(int K) {
+  if (sizeof(T) == 4) return true;
+  const int64_t mmas = (int64_t)(KIND == 1 ? PieceCount<T>::N : 1) * K / (KIND == 0 ? 64 : 32);
+  return mmas > (std::is_same<T, __half>::value ? 3072 : 16384);
+}
+
+template <int KIND, typename T, bool PROMOTE>
 aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s) {
   using Kd = MxKind<KIND>;
-  constexpr bool PROMOTE = sizeof(T) == 4;
   DeviceProps props;
   if (aiq_status_t st = current_device_props(&props)) return st;
-  AIQ_ENSURE_DYNAMIC_SMEM((mx_tc_kernel<KIND, T>), props.smem_optin);
+  AIQ_ENSURE_DYNAMIC_SMEM((mx_tc_kernel<KIND, T, PROMOTE>), props.smem_optin);
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return set_error(AIQ_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
 
@@ -834,10 +845,17 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   // cluster has its SM to itself: it asks for all of the shared memory.
   const size_t smem = p.cluster > 1 ? (size_t)props.smem_optin : (size_t)mx_smem_bytes(p);
   const int grid = p.cluster > 1 || p.tiles < n_sms ? p.tiles * p.cluster : n_sms;
-  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T>, dim3(grid), dim3(kMxTcThreads), smem, s, a_map, b_map, sa_map, sb_map, p,
+  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T, PROMOTE>, dim3(grid), dim3(kMxTcThreads), smem, s, a_map, b_map, sa_map, sb_map, p,
                                       g.bias, static_cast<T*>(g.y), g.y_stride));
   AIQ_LAUNCH_CHECK("mx_tc");
   return AIQ_OK;
+}
+
+template <int KIND, typename T>
+aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (!mx_promote<KIND, T>(g.K)) return launch_kind<KIND, T, false>(g, workspace, s);
+  return launch_kind<KIND, T, true>(g, workspace, s);
 }
 
 }  // namespace

@@ -108,3 +108,68 @@ def test_one_row_with_one_weight_per_channel(dtype):
     want = (x[0, at].double() * 2.0 ** (e.double() - 2) * (1 - 2 * sign)).to(dt)
     y = linear(codes, scales, None, x.cuda(), torch.full((1, n), float("nan"), dtype=dt, device="cuda"))
     assert torch.equal(y[0].cpu(), want)
+
+
+TABLE = [0, .5, 1, 1.5, 2, 3, 4, 6]
+
+
+def _positive(n, k, seed):
+    """Random codes without a sign, rows of k, and scale bytes around 2^-15, made on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 256, (n, -(-k // 128) * 64), dtype=torch.uint8, device="cuda", generator=g) & 0x77
+    at = 2 * torch.arange(codes.shape[1], device="cuda")
+    codes &= ((at < k).to(torch.uint8) * 0x0F) | ((at + 1 < k).to(torch.uint8) * 0xF0)
+    scales = torch.randint(111, 114, (n, -(-k // 512) * 16), dtype=torch.uint8, device="cuda", generator=g)
+    scales[:, -(-k // 32):] = 0
+    return codes, scales
+
+
+def _positive_sums(x, codes, scales, k):
+    """float64 x w^T for x [M][k] or (codes, scales), w as codes and scales without signs."""
+    table = torch.tensor(TABLE, dtype=torch.float64, device="cuda")
+
+    def part(c, s, a, b):
+        v = table[torch.stack((c[:, a // 2:b // 2] & 15, c[:, a // 2:b // 2] >> 4), 2).view(c.shape[0], -1).int()]
+        return v * torch.exp2(s[:, a // 32:-(-b // 32)].double() - 127).repeat_interleave(32, 1)[:, :v.shape[1]]
+    total = 0
+    for a in range(0, k, 32768):
+        b = min(a + 32768, -(-k // 32) * 32)
+        xs = part(*x, a, b) if isinstance(x, tuple) else torch.nn.functional.pad(x[:, a:b].double(), (0, b - min(b, k)))
+        total = total + xs @ part(codes, scales, a, b).t()
+    return total
+
+
+# Nothing cancels in sums of positive products, so what the additions drop adds up.  Up to 512 k at a time stay in the accumulator: 16 MMAs per
+# piece of x (8 with both microscaled), each of which drops less than 2^-23 of the sum so far; what leaves it is added in float32, K / 512
+# roundings of 2^-24 and 8 for splits and bias.  The mean error of R rounded results is below that plus 6 standard deviations of their own
+# rounding, which is at most eps / 2 either way: eps / 2 / sqrt(3 R).  (Halves below 2^-14 lie 2^-24 apart, the smallest normal number times eps:
+# half of that is what their rounding may take, whatever their size.  "matmul" with halves sums up to about 2^-19, "matmul up" to 2^-12.)
+@pytest.mark.parametrize("dtype,kind,n,k,m", [("f16", "linear", 2048, 131072, 520), ("f16", "linear", 256, 100001, 33), ("f16", "linear", 300, 40000, 130),
+                                              ("f16", "matmul", 2048, 200000, 520), ("f16", "matmul up", 2048, 200000, 520),
+                                              ("bf16", "linear", 1024, 300000, 300),
+                                              ("bf16", "linear", 130, 270000, 70), ("bf16", "matmul", 130, 1050000, 40),
+                                              ("f32", "linear", 10240, 20000, 40), ("f32", "matmul", 10240, 20000, 40)])
+def test_long_sums_of_positive_products(dtype, kind, n, k, m):
+    b, dt = binding(), TYPES[dtype]
+    codes, scales = _positive(n, k, 1)
+    few = torch.cat((torch.arange(min(n, 64)), torch.arange(max(n - 64, 64), n))).cuda()
+    y = torch.full((m, n), float("nan"), dtype=dt, device="cuda")
+    if kind == "linear":
+        g = torch.Generator(device="cuda").manual_seed(2)
+        x = (torch.rand((m, k), device="cuda", generator=g) * 2.0 ** -6).to(dt)
+        linear(codes, scales, None, x, y)
+    else:
+        x = _positive(m, k, 3)
+        x[1][:, : k // 32].sub_(8 if kind == "matmul" else 0)
+        b.aiq_mx_matmul(*x, codes, scales, None, k, y)
+    ref = _positive_sums(x, codes[few], scales[few], k)
+    e = (y[:, few].double() - ref) / ref
+    pieces = {"f32": 5, "f16": 3, "bf16": 2}[dtype]
+    chain = 16 * pieces if kind == "linear" else 8
+    sums = chain * 2.0 ** -23 + (k / 512 + 8) * 2.0 ** -24
+    if kind == "linear":
+        sums += 2.0 ** -(12 + 5 * pieces) * 32                        # x itself: 2^-(12 + 5 pieces) of the largest, which is below 32 of a block's sum
+    f = torch.finfo(dt)
+    half = torch.clamp(f.smallest_normal / ref, min=1) * f.eps / 2
+    assert (e.abs() <= sums + half * (1 + sums)).all(), e.abs().max()
+    assert abs(e.mean().item()) <= sums + 6 * half.max().item() / (3 * e.numel()) ** 0.5
