@@ -650,6 +650,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 // ---------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 256;
 constexpr int kSplitWords = 2;               // words of eight values per lane
+static_assert(kSplitWords % 2 == 0, "a warp takes whole groups of 512 k, as rows of scale bytes do: it writes all 16 of each");
 
 // A warp takes 512 values of one row, a lane eight at a time.  2,048 x 8192, the profiler's times behind a write of 200 MB, so with old
 // lines to write back on the way: bfloat16 18.3 us (68 MB; 18.9 with a 64-bit division for the row), half 22.7, float32 28.9.  With one word
@@ -680,10 +681,6 @@ mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int64_t M, i
       if ((lane & 3) == 0 && (word >> 2) < scale_row) sr[q * piece_scales + (word >> 2)] = (uint8_t)s;       // blocks behind K: zero
     });
   }
-  const int end = (word0 - lane + 32 * kSplitWords) >> 2;      // the row's last segment: scale bytes behind its own blocks
-  if ((word0 - lane) + 32 * kSplitWords >= words && end + lane < scale_row)
-#pragma unroll
-    for (int q = 0; q < PieceCount<T>::N; ++q) sr[q * piece_scales + end + lane] = 0;
 }
 
 inline int mx_pieces(int dtype) { return dtype == AIQ_DTYPE_F32 ? 5 : dtype == AIQ_DTYPE_F16 ? 3 : 2; }

@@ -173,3 +173,35 @@ def test_long_sums_of_positive_products(dtype, kind, n, k, m):
     half = torch.clamp(f.smallest_normal / ref, min=1) * f.eps / 2
     assert (e.abs() <= sums + half * (1 + sums)).all(), e.abs().max()
     assert abs(e.mean().item()) <= sums + 6 * half.max().item() / (3 * e.numel()) ** 0.5
+
+
+GUARD = 4096
+
+
+@pytest.mark.parametrize("start", [0x00, 0xFF])
+def test_one_workspace_for_every_shape_and_type(start):
+    """Calls of several shapes and types in turn on one workspace, filled with 0xFF (as a scale byte: NaN) or zeros before the first and never
+    again: each gives what it gives on a fresh one, and nothing behind the bytes it asks for changes."""
+    b = binding()
+    calls = [("f32", 700, 640, 257), ("bf16", 129, 4100, 17), ("f16", 5671, 609, 37), ("bf16", 512, 1025, 300), ("f32", 200, 6000, 33), ("f16", 260, 3100, 129),
+             ("f32", 1001, 1300, 20), ("bf16", 9500, 2176, 5), ("f16", 300, 40000, 60), ("f32", 8192, 4096, 1), ("bf16", 700, 1500, 2048)]
+    made = []
+    for kind, n, k, m in calls:
+        codes, scales = held(weights(n, k, n + k))
+        x = activations(m, k, TYPES[kind], m + k)
+        size = b.aiq_mx_linear_workspace_bytes(n, k, m, TYPES[kind])
+        y = torch.full((m, n), float("nan"), dtype=TYPES[kind], device="cuda")
+        if size:
+            ws = torch.full((size,), 0xFF - start, dtype=torch.uint8, device="cuda")
+            b.aiq_mx_linear(codes, scales, None, x, y, workspace=ws)
+            check(y[:, :130], x.double().cpu().numpy(), values(codes[:130], scales[:130], k), None, TYPES[kind], kind)
+            made.append((kind, codes, scales, x, y, size))
+    assert len(made) >= 10
+    ws = torch.full((max(c[-1] for c in made) + GUARD,), start, dtype=torch.uint8, device="cuda")
+    for order in (made, made[::-1]):
+        for kind, codes, scales, x, y, size in order:
+            behind = ws[size:].clone()
+            out = torch.full_like(y, float("nan"))
+            b.aiq_mx_linear(codes, scales, None, x, out, workspace=ws[:size])
+            assert torch.equal(out, y), (kind, y.shape)
+            assert torch.equal(ws[size:], behind)
