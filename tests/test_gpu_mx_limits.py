@@ -205,3 +205,66 @@ def test_one_workspace_for_every_shape_and_type(start):
             b.aiq_mx_linear(codes, scales, None, x, out, workspace=ws[:size])
             assert torch.equal(out, y), (kind, y.shape)
             assert torch.equal(ws[size:], behind)
+
+
+def _one_weight_per_channel(n, k, seed):
+    """Channels with one element other than zero, +-1, 2 or 4 times 2^-2: (codes, scales, its k, its value)."""
+    g = torch.Generator().manual_seed(seed)
+    # every k in turn, the last ones first: the ends of blocks, of 128, 512 and of K are all met
+    at = (k - 1 - torch.arange(n) * max(1, k // n)) % k
+    e, sign = torch.randint(0, 3, (n,), generator=g), torch.randint(0, 2, (n,), generator=g)
+    codes = torch.zeros((n, -(-k // 128) * 128), dtype=torch.uint8)
+    codes[torch.arange(n), at] = (2 * (e + 1) + 8 * sign).to(torch.uint8)
+    scales = torch.zeros((n, -(-k // 512) * 16), dtype=torch.uint8)
+    scales[:, : -(-k // 32)] = 125
+    return (codes[:, 0::2] | (codes[:, 1::2] << 4)).cuda(), scales.cuda(), at, 2.0 ** (e.double() - 2) * (1 - 2 * sign)
+
+
+# With one weight other than zero there is nothing to add up: y is x times a power of two, and float32, half and bfloat16 hold that.  x has every
+# bit of its type's mantissa and lies within 2^-8 of its block's largest, so its pieces hold it: 2^-22 of that one at bfloat16 (8 bits below 2^-8),
+# 2^-27 at half (11), 2^-37 at float32 (24).  A piece left out, or scaled or placed wrongly, shows in the last bits of some channel.
+# In turn: rows of x beside each other (pieces stacked), above each other, split K ranges, whole tiles and halves of them, the few-row kernel.
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n,k,m", [(1100, 1000, 20), (609, 4100, 37), (200, 6000, 33), (700, 640, 257), (2500, 520, 2200), (1290, 650, 3500), (257, 9000, 70),
+                                   (1001, 3001, 48), (9500, 520, 16), (128, 8192, 600), (300, 33000, 40), (64, 320, 9), (100, 3001, 3), (2050, 640, 1)])
+def test_one_weight_per_channel_is_exact(dtype, n, k, m):
+    dt = TYPES[dtype]
+    codes, scales, at, w = _one_weight_per_channel(n, k, n)
+    g = torch.Generator().manual_seed(k + m)
+    x = (1 + torch.rand((m, k), generator=g)) * torch.exp2(torch.randint(-4, 4, (m, k), generator=g).float())
+    x = (x * (1 - 2 * torch.randint(0, 2, (m, k), generator=g))).to(dt)
+    y = linear(codes, scales, None, x.cuda(), torch.full((m, n), float("nan"), dtype=dt, device="cuda"))
+    assert torch.equal(y.cpu(), (x[:, at].double() * w).to(dt))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n,k,m", [(1100, 1000, 20), (200, 6000, 33), (700, 640, 257), (2500, 520, 2200), (1290, 650, 3500), (128, 8192, 600), (300, 200000, 40),
+                                   (64, 320, 9), (2050, 640, 1)])
+def test_one_weight_per_channel_is_exact_with_both_microscaled(dtype, n, k, m):
+    b, dt = binding(), TYPES[dtype]
+    codes, scales, at, w = _one_weight_per_channel(n, k, n)
+    ac, as_ = held(activations(m, k, torch.float32, k + m))
+    x = torch.from_numpy(values(ac, as_, k))
+    y = torch.full((m, n), float("nan"), dtype=dt, device="cuda")
+    b.aiq_mx_matmul(ac, as_, codes, scales, None, k, y)
+    assert torch.equal(y.cpu(), (x[:, at] * w).float().to(dt))
+
+
+# How far float32 sums are off in the mean.  An MMA drops what is below the last place of the sum so far, up to a unit of 2^-23 of it, 0.58 of one in
+# root mean square.  Of the 16 MMAs of a piece and 512 k only the largest piece's meet sums of full size (the smaller pieces come first, each
+# 2^-5 of the next), the j-th of them sqrt(j / 16) of it: 0.58 (1 + 2^-5 + ...) sum_j sqrt(j / 16) < 7 units, if all add up.  From set to set the sums'
+# signs are as good as independent, as are the K / 512 roundings of half a unit behind them.  With s = sqrt(sum (x w)^2), the standard
+# deviation of y: below (7 + sqrt(K / 512) / 2) 2^-23 s.  (What one accumulator for all of K costs shows in the long sums above, the pieces in
+# the single weights.)
+@pytest.mark.parametrize("n,k,m", [(4096, 4096, 256), (10240, 20000, 40), (2048, 8192, 2048)])
+def test_float32_sums_in_the_mean(n, k, m):
+    codes, scales = held(weights(n, k, n + k))
+    x = activations(m, k, torch.float32, m + k)
+    y = linear(codes, scales, None, x, torch.full((m, n), float("nan"), device="cuda"))
+    few = torch.cat((torch.arange(64), torch.arange(n - 64, n))).cuda()
+    w, xd = _rows_of(codes[few], scales[few], k), x.double()
+    e = y[:, few].double() - xd @ w.t()
+    s = ((xd * xd) @ (w * w).t()).sqrt()
+    rms = (e / s).square().mean().sqrt().item()
+    print(f"{n} x {k}, {m} rows: {rms:.3g}, allowed {(7 + (k / 512) ** 0.5 / 2) * 2.0 ** -23:.3g}")
+    assert rms <= (7 + (k / 512) ** 0.5 / 2) * 2.0 ** -23
