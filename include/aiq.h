@@ -201,7 +201,8 @@ aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales, int rows, 
  * sizes, so a row's last bits depend on how many rows come with it.  `workspace`: device, 16-byte aligned,
  * aiq_mx_linear_workspace_bytes(...) bytes (0 where one of the first
  * two is chosen or an argument is out of range), not used by two calls at a time.  NULL: the first two, whatever the size.
- * Every wait inside the tensor-core kernel is bounded (about 2 s); should one run out, the tile of y becomes NaN. */
+ * The waits of the tensor-core kernel for copies, scales and sums are bounded (about 2 s); should one run out, that block's part of y becomes NaN.
+ * (Tensor memory, and the other blocks of a cluster, are waited for as long as it takes the kernels that hold the one and the others to end.) */
 size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype);
 aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
                            int M, int64_t x_stride, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,
@@ -211,6 +212,10 @@ aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* b
  * kind::mxf4 on the tensor cores, which take codes and scales as they are stored; the kernels for small matrices and for a single row as above. */
 aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales, int M, const void* b_codes, const void* b_scales, int N,
                            const float* bias, int K, void* y, int dtype, int64_t y_stride, void* stream);
+/* Test aid for what happens when a wait runs out, beside aiq_debug_expire_wait: the next aiq_mx_linear or aiq_mx_matmul of the calling thread that
+ * runs on the tensor cores holds one kind of arrival back and gives its waits up after `limit_cycles` SM clocks (at most 2e9; 0: takes the
+ * request back).  It ends in an ordinary way, with NaN in all of y. */
+aiq_status_t aiq_debug_mx_expire_wait(int64_t limit_cycles);
 
 /* ------------------------------------------------------------------------------------
  * Model description.  Layers are listed in scheme order: entry i of a scheme is the

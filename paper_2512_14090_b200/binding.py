@@ -27,7 +27,7 @@ EXPORTS = [
     "aiq_eval_schemes", "aiq_set_eval_options", "aiq_set_fusion", "aiq_set_small_pass_images", "aiq_quantize_layer_per_tensor", "aiq_set_scale_granularity", "aiq_last_call_stats", "aiq_scheme_ai",
     "aiq_profile_start", "aiq_profile_stop", "aiq_forward_static",
     "aiq_mx_row_bytes", "aiq_mx_scale_row_bytes", "aiq_mx_quantize", "aiq_mx_dequantize", "aiq_mx_linear_workspace_bytes",
-    "aiq_mx_linear", "aiq_mx_matmul",
+    "aiq_mx_linear", "aiq_mx_matmul", "aiq_debug_mx_expire_wait",
     "aiq_set_compute_path", "aiq_model_status", "aiq_debug_expire_wait", "aiq_search_greedy", "aiq_search_coordinate_descent",
 ]
 
@@ -101,6 +101,8 @@ def _load():
     lib.aiq_mx_linear_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.aiq_mx_linear.restype = i32
     lib.aiq_mx_linear.argtypes = [vp, vp, vp, i32, i32, vp, i32, i32, i64, vp, i64, vp, sz, vp]
+    lib.aiq_debug_mx_expire_wait.restype = i32
+    lib.aiq_debug_mx_expire_wait.argtypes = [i64]
     lib.aiq_mx_matmul.restype = i32
     lib.aiq_mx_matmul.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, i32, i64, vp]
     lib.aiq_model_bytes.restype = sz
@@ -416,6 +418,10 @@ def aiq_mx_matmul(a_codes, a_scales, b_codes, b_scales, bias, K, y, stream=None)
                                bias.data_ptr() if bias is not None else None, int(K), y.data_ptr(), dtype, y_stride, s)
     if status:
         _check(status)
+
+
+def aiq_debug_mx_expire_wait(limit_cycles):
+    _check(lib.aiq_debug_mx_expire_wait(int(limit_cycles)))
 
 
 def aiq_set_eval_options(chunk=0, share_prefix=True):

@@ -873,3 +873,10 @@ extern "C" aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales,
   if (mx_rows_pay(N, K, M, M == 1 ? 25 : 22)) return aiq::launch_mx_product_rows(p, (cudaStream_t)stream);
   return aiq::launch_mx_product_tc(p, nullptr, (cudaStream_t)stream);
 }
+
+extern "C" aiq_status_t aiq_debug_mx_expire_wait(int64_t limit_cycles) {
+  if (limit_cycles < 0 || limit_cycles > 2000000000ll)
+    return set_error(AIQ_ERR_INVALID_ARG, "aiq_debug_mx_expire_wait: limit_cycles=%lld outside [0, 2e9]", (long long)limit_cycles);
+  aiq::mx_tc_expire_next(limit_cycles);
+  return AIQ_OK;
+}

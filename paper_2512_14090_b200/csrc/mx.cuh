@@ -39,6 +39,7 @@ aiq_status_t launch_mx_product_rows(const MxProduct& p, cudaStream_t s);
 // tensor cores (mx_tc.cu); with x not microscaled: needs the workspace, for x as eight-bit pieces
 size_t mx_tc_workspace_bytes(int K, int M, int dtype);
 aiq_status_t launch_mx_product_tc(const MxProduct& p, void* workspace, cudaStream_t s);
+void mx_tc_expire_next(int64_t limit_cycles);      // see aiq_debug_mx_expire_wait
 
 // ---- device helpers -------------------------------------------------------------------
 // 2^(s - 127) as a float; NaN for 255

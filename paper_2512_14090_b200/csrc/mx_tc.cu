@@ -70,6 +70,8 @@ struct MxTcParams {
   int b_cols;               // scale columns of a B operand (a multiple of 4)
   int sf_col, sf_group;     // first scale column, columns per 128 k
   int tmem_cols;
+  int hold;                 // 1: no scale words are reported as written, so that waits run out (aiq_debug_mx_expire_wait)
+  int limit;                // of a wait, in units of 1024 cycles
 };
 
 // tile `t` of a launch
@@ -148,6 +150,10 @@ __device__ __forceinline__ void tma_load_3d_elect(uint32_t dst, const CUtensorMa
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 
+// The limit lies behind the abort flag in shared memory: read from there it costs a wait that does not run out nothing; as a kernel parameter
+// it took 1.5 to 2 % (matmul 8192 x 8192, 2,048 rows 63.7 -> 64.7 us).
+__device__ __forceinline__ long long mx_limit(volatile int* abort_flag) { return (long long)abort_flag[1] << 10; }
+
 // Bounded wait of the issuing warp, in line and decided by votes: a call would have everything that lives across it moved out of
 // the uniform registers, and an MMA whose operands are not in those takes 180 cycles to issue instead of 40.
 __device__ __forceinline__ bool mbar_wait_uniform(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -156,12 +162,21 @@ __device__ __forceinline__ bool mbar_wait_uniform(uint32_t bar, uint32_t parity,
   for (uint32_t i = 0; i < kSpinLimit; ++i) {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     if ((i & 63u) == 63u) {
-      const bool over = clock64() - t0 > kWaitLimitCycles;
+      const bool over = clock64() - t0 > mx_limit(abort_flag);
       if (__any_sync(0xffffffffu, over || *abort_flag != 0)) break;
     }
   }
   *abort_flag = 1;
   return false;
+}
+
+// The other warps'.
+static __device__ __noinline__ bool mx_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return mbar_wait_for(bar, parity, abort_flag, nullptr, mx_limit(abort_flag));
+}
+__device__ __forceinline__ bool mx_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mx_wait_slow(bar, parity, abort_flag));
 }
 
 // A ring of copies as its producer sees it: wait for the slot, remember the copy; drain() before the CTA may end.
@@ -297,7 +312,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     const int rings = 2 * (a_stages + b_stages) + kMxScaleStages;
     for (int i = lane; i < rings + kMxScaleStages + 9; i += 32)
       mbar_init(a_full + 8 * i, i >= rings && i < rings + kMxScaleStages + 2 ? 4 : i >= rings + kMxScaleStages + 6 && i < rings + kMxScaleStages + 8 ? 8 : 1);
-    if (lane == 0) *s_abort = 0;
+    if (lane == 0) { s_abort[0] = 0; s_abort[1] = p.limit; }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
     if (chunks > 0 && first < p.tiles) tma_fill_2d(smem_u32(sring), &sa_map, s_full, (uint32_t)((128 + (p.stack ? p.rows : mx_tile(p, first).Mt * units)) * 16), c_begin / Kd::CPS * 16, a_n0);
@@ -317,7 +332,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
 
   if (warp == 0) {
     while (chunks > 0 && a_tile < p.tiles) {
-      alive = mbar_wait_warp(a_empty + 8 * ar.stage, ar.phase ^ 1u, s_abort, nullptr);
+      alive = mx_wait(a_empty + 8 * ar.stage, ar.phase ^ 1u, s_abort);
       if (!alive) break;
       send_a();
     }
@@ -331,7 +346,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       for (int c0 = c_begin; c0 < c_end && alive; c0 += Kd::CPS)
         for (int u = units - 1; u >= 0 && alive; --u)
           for (int c = c0; c < min(c0 + Kd::CPS, c_end); ++c) {
-            alive = mbar_wait_warp(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+            alive = mx_wait(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort);
             if (!alive) break;
             const uint32_t dst = smem_u32(bring) + r.stage * b_unit;
             tma_fill_3d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)bytes, c * 128, at.m0, u);
@@ -347,7 +362,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       const MxTile at = mx_tile(p, tile);
       const int boxes = at.Mt > p.box ? 2 : 1, bytes = (128 + (p.stack ? p.rows : at.Mt * units)) * 16;
       for (int s = 0; s < supers; ++s) {
-        alive = mbar_wait_warp(s_empty + 8 * r.stage, r.phase ^ 1u, s_abort, nullptr);
+        alive = mx_wait(s_empty + 8 * r.stage, r.phase ^ 1u, s_abort);
         if (!alive) break;
         const uint32_t dst = smem_u32(sring) + r.stage * scale_tile, bar = s_full + 8 * r.stage;
         const int byte = (c_begin / Kd::CPS + s) * 16;
@@ -430,7 +445,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     uint32_t stage = 0, phase = 0;
     for (int s = 0; s < sets; ++s) {
       const uint32_t tb = s & 1, tph = (s >> 1) & 1;
-      alive = mbar_wait_warp(s_full + 8 * stage, phase, s_abort, nullptr) && mbar_wait_warp(t_empty + 8 * tb, tph ^ 1u, s_abort, nullptr);
+      alive = mx_wait(s_full + 8 * stage, phase, s_abort) && mx_wait(t_empty + 8 * tb, tph ^ 1u, s_abort);
       if (!alive) break;
       tc_fence_after();
       const uint32_t src = smem_u32(sring) + stage * scale_tile + lane * 16;
@@ -448,7 +463,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(s_empty + 8 * stage);
-        mbar_arrive(t_full + 8 * tb);
+        if (!p.hold) mbar_arrive(t_full + 8 * tb);
       }
       if (++stage == kMxScaleStages) { stage = 0; phase ^= 1u; }
     }
@@ -483,7 +498,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         for (int i = 0; i < 64; ++i) acc[i] = 0.f;
         for (int s = 0; s < supers; ++s, ++sets) {
           const uint32_t tb = sets & 1, tph = (sets >> 1) & 1;
-          alive = mbar_wait_warp(d_full + 8 * tb, tph, s_abort, nullptr);
+          alive = mx_wait(d_full + 8 * tb, tph, s_abort);
           if (!alive) break;
           tc_fence_after();
           for (int q = copies - 1; q >= 0; --q) {              // the smallest pieces first
@@ -520,7 +535,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       } else {
         // Not unrolled: code that a block runs once per tile comes from far away (unrolled, 16 columns took 1,000 cycles).
         const uint32_t db = p.d_bufs == 2 ? done & 1 : 0, dph = (p.d_bufs == 2 ? done >> 1 : done) & 1;
-        if (supers > 0) alive = mbar_wait_warp(d_full + 8 * db, dph, s_abort, nullptr);
+        if (supers > 0) alive = mx_wait(d_full + 8 * db, dph, s_abort);
         if (!alive) break;
         tc_fence_after();
         T* out = dst;
@@ -724,6 +739,8 @@ bool mx_promote(int K) {
   return mmas > (std::is_same<T, __half>::value ? 3072 : 16384);
 }
 
+thread_local long long mx_expire = 0;          // cycles: the next product of this thread holds an arrival back, 0: none does
+
 template <int KIND, typename T, bool PROMOTE>
 aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s) {
   using Kd = MxKind<KIND>;
@@ -735,6 +752,8 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
 
   MxTcParams p = {};
   p.N = g.N; p.M = g.M;
+  p.limit = (int)((mx_expire ? mx_expire : kWaitLimitCycles) >> 10);
+  p.hold = mx_expire != 0;
   p.pieces = KIND == 1 ? PieceCount<T>::N : 1;
   p.n_chunks = (g.K + Kd::CHUNK - 1) / Kd::CHUNK;
   const int n_super = (g.K + kMxSuper - 1) / kMxSuper, row_blocks = (g.N + 127) / 128, n_sms = props.n_sms;
@@ -861,8 +880,11 @@ size_t mx_tc_workspace_bytes(int K, int M, int dtype) {
   return align_up((size_t)mx_pieces(dtype) * M * (size_t)(mx_plane_row(K) + mx_scale_row_bytes(K)), 16);
 }
 
+void mx_tc_expire_next(int64_t limit_cycles) { mx_expire = limit_cycles; }
+
 aiq_status_t launch_mx_product_tc(const MxProduct& p, void* workspace, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
+  struct Once { ~Once() { mx_expire = 0; } } once;
   switch (p.dtype) {
     case AIQ_DTYPE_F32: return p.x ? launch_kind<1, float>(p, ws, s) : launch_kind<0, float>(p, ws, s);
     case AIQ_DTYPE_F16: return p.x ? launch_kind<1, __half>(p, ws, s) : launch_kind<0, __half>(p, ws, s);

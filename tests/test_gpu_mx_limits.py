@@ -268,3 +268,46 @@ def test_float32_sums_in_the_mean(n, k, m):
     rms = (e / s).square().mean().sqrt().item()
     print(f"{n} x {k}, {m} rows: {rms:.3g}, allowed {(7 + (k / 512) ** 0.5 / 2) * 2.0 ** -23:.3g}")
     assert rms <= (7 + (k / 512) ** 0.5 / 2) * 2.0 ** -23
+
+
+# In turn: whole tiles written by their block, a cluster that writes its sums into each other's shared memory, one that reads them from there.
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "mx"])
+@pytest.mark.parametrize("n,k,m", [(1290, 650, 3500), (200, 6000, 33), (128, 8192, 600)])
+def test_a_wait_that_runs_out_ends_in_nan(kind, n, k, m):
+    """An arrival held back, a limit of about a millisecond: the kernel ends by itself with NaN in y; the next call is as ever."""
+    b, dt = binding(), TYPES.get(kind, torch.float32)
+    codes, scales = held(weights(n, k, 1))
+    x = activations(m, k, dt, 2)
+    xc, xs = held(x)
+    size = b.aiq_mx_linear_workspace_bytes(n, k, m, dt)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def call():
+        y = torch.zeros((m, n), dtype=dt, device="cuda")
+        if kind == "mx":
+            b.aiq_mx_matmul(xc, xs, codes, scales, None, k, y)
+        else:
+            b.aiq_mx_linear(codes, scales, None, x, y, workspace=ws)
+        return y
+    want = call()
+    assert torch.isfinite(want).all()
+    b.aiq_debug_mx_expire_wait(2_000_000)
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    y = call()
+    end.record()
+    torch.cuda.synchronize()
+    assert torch.isnan(y).all()
+    assert start.elapsed_time(end) < 1000.0
+    assert torch.equal(call(), want)
+    b.aiq_debug_mx_expire_wait(2_000_000)
+    b.aiq_debug_mx_expire_wait(0)                                      # taken back
+    assert torch.equal(call(), want)
+
+
+def test_limits_that_are_refused():
+    b = binding()
+    for limit in (-1, 2_000_000_001):
+        with pytest.raises(b.AiqError) as e:
+            b.aiq_debug_mx_expire_wait(limit)
+        assert e.value.status == b.ERR_INVALID_ARG
