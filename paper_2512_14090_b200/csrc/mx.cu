@@ -801,6 +801,7 @@ extern "C" size_t aiq_mx_scale_row_bytes(int K) { return K > 0 ? (size_t)aiq::mx
 
 extern "C" aiq_status_t aiq_mx_quantize(const void* x, int dtype, int rows, int K, int64_t x_stride, void* codes_out,
                                         void* scales_out, void* stream) {
+  if (rows == 1) x_stride = K;                 // ignored
   if (aiq_status_t st = mx_check("aiq_mx_quantize", codes_out, scales_out, rows, K)) return st;
   if (aiq_status_t st = mx_check_rows("aiq_mx_quantize", x, dtype, x_stride)) return st;
   if (aiq_status_t st = aiq::check_device_sm100()) return st;
@@ -810,6 +811,7 @@ extern "C" aiq_status_t aiq_mx_quantize(const void* x, int dtype, int rows, int 
 
 extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales, int rows, int K, int dtype, void* y, int64_t y_stride,
                                           void* stream) {
+  if (rows == 1) y_stride = K;
   if (aiq_status_t st = mx_check("aiq_mx_dequantize", codes, scales, rows, K)) return st;
   if (aiq_status_t st = mx_check_out("aiq_mx_dequantize", y, dtype, rows, K, y_stride)) return st;
   if (aiq_status_t st = aiq::check_device_sm100()) return st;
@@ -836,6 +838,7 @@ extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, con
                                       void* stream) {
   if (aiq_status_t st = mx_check("aiq_mx_linear", codes, scales, N, K)) return st;
   if (M <= 0 || M > kMxMost) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear: M=%d", M);
+  if (M == 1) { x_stride = K; y_stride = N; }
   if (aiq_status_t st = mx_check_rows("aiq_mx_linear", x, dtype, x_stride)) return st;
   if (aiq_status_t st = mx_check_out("aiq_mx_linear", y, dtype, M, N, y_stride)) return st;
   if (aiq_status_t st = mx_check_bias("aiq_mx_linear", bias)) return st;
@@ -859,6 +862,7 @@ extern "C" aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales,
                                       const float* bias, int K, void* y, int dtype, int64_t y_stride, void* stream) {
   if (aiq_status_t st = mx_check("aiq_mx_matmul", a_codes, a_scales, M, K)) return st;
   if (aiq_status_t st = mx_check("aiq_mx_matmul", b_codes, b_scales, N, K)) return st;
+  if (M == 1) y_stride = N;
   if (aiq_status_t st = mx_check_out("aiq_mx_matmul", y, dtype, M, N, y_stride)) return st;
   if (aiq_status_t st = mx_check_bias("aiq_mx_matmul", bias)) return st;
   if (aiq_status_t st = aiq::check_device_sm100()) return st;

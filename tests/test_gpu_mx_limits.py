@@ -311,3 +311,25 @@ def test_limits_that_are_refused():
         with pytest.raises(b.AiqError) as e:
             b.aiq_debug_mx_expire_wait(limit)
         assert e.value.status == b.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("stride", [-1, 0, 1 << 62])
+def test_the_stride_of_a_single_row_is_ignored(stride):
+    b, n, k = binding(), 300, 700
+    codes, scales = held(weights(n, k, 1))
+    for kind, dt in TYPES.items():
+        code = b._dtype(dt)
+        x = activations(1, k, dt, 2)
+        xc, xs = held(x)
+        c, s = torch.zeros_like(xc), torch.zeros_like(xs)
+        assert b.lib.aiq_mx_quantize(x.data_ptr(), code, 1, k, stride, c.data_ptr(), s.data_ptr(), None) == b.OK
+        wide = torch.full((1, k), float("nan"), dtype=dt, device="cuda")
+        assert b.lib.aiq_mx_dequantize(c.data_ptr(), s.data_ptr(), 1, k, code, wide.data_ptr(), stride, None) == b.OK
+        y, z = (torch.full((1, n), float("nan"), dtype=dt, device="cuda") for _ in range(2))
+        assert b.lib.aiq_mx_linear(codes.data_ptr(), scales.data_ptr(), None, n, k, x.data_ptr(), code, 1, stride, y.data_ptr(), stride, None, 0, None) == b.OK
+        assert b.lib.aiq_mx_matmul(xc.data_ptr(), xs.data_ptr(), 1, codes.data_ptr(), scales.data_ptr(), n, None, k, z.data_ptr(), code, stride, None) == b.OK
+        torch.cuda.synchronize()
+        assert torch.equal(c, xc) and torch.equal(s, xs)
+        assert torch.equal(wide.cpu(), torch.from_numpy(values(c, s, k)).to(dt))
+        check(y, x.double().cpu().numpy(), values(codes, scales, k), None, dt, kind)
+        check(z, values(xc, xs, k), values(codes, scales, k), None, dt, "mx")
