@@ -68,6 +68,14 @@ class LayerWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("W", "gamma", "beta", "mean", "var", "bias")]
 
 
+class _Int:
+    """An `int` argument: out of its range, the smallest one, which every entry point refuses (c_int would keep the low 32 bits)."""
+
+    @staticmethod
+    def from_param(value):
+        return C.c_int(value if -2 ** 31 <= value < 2 ** 31 else -2 ** 31)
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is missing: build it with "
@@ -88,23 +96,23 @@ def _load():
     lib.aiq_qlinear.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, sz, vp]
     lib.aiq_qlinear_workspace_bytes.restype = sz
     lib.aiq_qlinear_workspace_bytes.argtypes = [i32, i32, i32, i32]
-    i64 = C.c_int64
+    i64, n32 = C.c_int64, _Int
     lib.aiq_mx_row_bytes.restype = sz
-    lib.aiq_mx_row_bytes.argtypes = [i32]
+    lib.aiq_mx_row_bytes.argtypes = [n32]
     lib.aiq_mx_scale_row_bytes.restype = sz
-    lib.aiq_mx_scale_row_bytes.argtypes = [i32]
+    lib.aiq_mx_scale_row_bytes.argtypes = [n32]
     lib.aiq_mx_quantize.restype = i32
-    lib.aiq_mx_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
+    lib.aiq_mx_quantize.argtypes = [vp, n32, n32, n32, i64, vp, vp, vp]
     lib.aiq_mx_dequantize.restype = i32
-    lib.aiq_mx_dequantize.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp]
+    lib.aiq_mx_dequantize.argtypes = [vp, vp, n32, n32, n32, vp, i64, vp]
     lib.aiq_mx_linear_workspace_bytes.restype = sz
-    lib.aiq_mx_linear_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.aiq_mx_linear_workspace_bytes.argtypes = [n32, n32, n32, n32]
     lib.aiq_mx_linear.restype = i32
-    lib.aiq_mx_linear.argtypes = [vp, vp, vp, i32, i32, vp, i32, i32, i64, vp, i64, vp, sz, vp]
+    lib.aiq_mx_linear.argtypes = [vp, vp, vp, n32, n32, vp, n32, n32, i64, vp, i64, vp, sz, vp]
     lib.aiq_debug_mx_expire_wait.restype = i32
     lib.aiq_debug_mx_expire_wait.argtypes = [i64]
     lib.aiq_mx_matmul.restype = i32
-    lib.aiq_mx_matmul.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, i32, i64, vp]
+    lib.aiq_mx_matmul.argtypes = [vp, vp, n32, vp, vp, n32, vp, n32, vp, n32, i64, vp]
     lib.aiq_model_bytes.restype = sz
     lib.aiq_model_bytes.argtypes = [C.POINTER(ArchDesc)]
     lib.aiq_model_create.restype = i32
