@@ -333,3 +333,29 @@ def test_the_stride_of_a_single_row_is_ignored(stride):
         assert torch.equal(wide.cpu(), torch.from_numpy(values(c, s, k)).to(dt))
         check(y, x.double().cpu().numpy(), values(codes, scales, k), None, dt, kind)
         check(z, values(xc, xs, k), values(codes, scales, k), None, dt, "mx")
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("n,k,m", [(300, 700, 1), (1100, 1500, 70), (1100, 1000, 1)])
+def test_calls_through_ctypes(monkeypatch, dtype, n, k, m):
+    """The four calls on the way that the binding takes where its CPython module is not built: the same bits."""
+    b, dt = binding(), TYPES[dtype]
+    assert b._mxcall is not b.lib, "the module is built where the tests run"
+    w, x = weights(n, k, 1), activations(m, k, dt, 2)
+    bias = torch.randn(n, generator=torch.Generator().manual_seed(3)).cuda()
+
+    def run():
+        codes, scales = held(w)
+        xc, xs = held(x)
+        back = torch.empty((n, k), dtype=dt, device="cuda")
+        b.aiq_mx_dequantize(codes, scales, back)
+        y = linear(codes, scales, bias, x, torch.empty((m, n), dtype=dt, device="cuda"))
+        z = torch.empty((m, n), dtype=dt, device="cuda")
+        b.aiq_mx_matmul(xc, xs, codes, scales, bias, k, z)
+        return codes, scales, xc, xs, back, y, z
+    want = run()
+    monkeypatch.setattr(b, "_mxcall", b.lib)
+    for got, w_ in zip(run(), want):
+        assert torch.equal(got, w_)
+    with pytest.raises(b.AiqError):
+        b.aiq_mx_dequantize(want[0], want[1], torch.empty((1, k), dtype=dt, device="cuda").expand(n, k))
