@@ -321,6 +321,8 @@ def _mx_held(codes, scales, k):
     """The rows of k values each that codes and scales hold."""
     if not codes.is_cuda or not scales.is_cuda:
         raise ValueError("expected CUDA tensors")
+    if codes.dim() != 2:
+        raise ValueError(f"expected codes of bytes, a row per row of values, not {tuple(codes.shape)}")
     rows = codes.shape[0]
     want = (rows, (k + 127) // 128 * 64), (rows, (k + 511) // 512 * 16)
     if (tuple(codes.shape), tuple(scales.shape)) != want or codes.element_size() != 1 or scales.element_size() != 1:

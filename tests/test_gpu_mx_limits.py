@@ -359,3 +359,16 @@ def test_calls_through_ctypes(monkeypatch, dtype, n, k, m):
         assert torch.equal(got, w_)
     with pytest.raises(b.AiqError):
         b.aiq_mx_dequantize(want[0], want[1], torch.empty((1, k), dtype=dt, device="cuda").expand(n, k))
+
+
+def test_codes_that_are_no_matrix():
+    b = binding()
+    codes, scales = held(weights(8, 64, 1))
+    x, y = activations(2, 64, torch.float32, 2), torch.empty((2, 8), device="cuda")
+    for bad in (codes[0, 0], codes[0], codes[None]):
+        with pytest.raises(ValueError):
+            b.aiq_mx_linear(bad, scales, None, x, y)
+        with pytest.raises(ValueError):
+            b.aiq_mx_quantize(x, bad, scales)
+        with pytest.raises(ValueError):
+            b.aiq_mx_matmul(codes, scales, bad, scales, None, 64, y)
