@@ -401,7 +401,8 @@ def aiq_mx_linear_workspace_bytes(N, K, M, dtype):
 
 
 def aiq_mx_linear(codes, scales, bias, x, y, workspace=None, stream=None):
-    """y [M][N] = x [M][K] * W^T + bias; W [N][K] as codes and scales, x and y of one type, bias float32 [N] or None."""
+    """y [M][N] = x [M][K] * W^T + bias; W [N][K] as codes and scales, x and y of one type, bias float32 [N] or None.  workspace: a tensor of
+    aiq_mx_linear_workspace_bytes(N, K, M, x.dtype) bytes; without one large products leave the tensor cores and take up to 100 times as long."""
     key = (codes.shape, scales.shape, x.shape, y.shape, x.stride(), y.stride(), x.dtype, y.dtype, codes.dtype, scales.dtype,
            codes.is_contiguous(), scales.is_contiguous(), (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None)
     n, k, dtype, m, x_stride, y_stride = _mx_plans.get(key) or _mx_plan(key, _mx_check_linear, codes, scales, bias, x, y)

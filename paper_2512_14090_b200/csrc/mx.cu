@@ -437,14 +437,17 @@ aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
 //     when it becomes a float32.
 //   What the planes cannot hold, the last bits of values below 2^-15 (bfloat16) or 2^-20 (half) of the block's largest, is multiplied value
 //     by value in float32 (one_rest): in normally distributed data one value in twenty thousand or fewer.
-// Bound by instruction issue: 110 to 120 a block and lane, issue slots 65 to 75 % busy, 60 % of them in the integer pipe.  On the device,
-// float kernel or tensor cores | this one, weights from memory: bfloat16 2000 x 2000 4.7 | 3.7 us, 8192 x 1024 6.0 | 4.7,
-// 1024 x 8192 6.0 | 4.7, 4096 x 4096 9.3 | 6.4; half, 4096 x 4096 8.5 | 6.7; microscaled 2000 x 2000 4.8 | 2.7, 4096 x 4096 7.2 | 4.8.
-// Few channels leave SMs without work: 70 x 16500 5.3 | 5.9.  Rounding what the planes cannot hold away instead took as long; finding it with
+// Bound by instruction issue: 110 to 120 a block and lane, issue slots 59 % busy and the integer pipe 50 % (28000 x 8192, bfloat16, 46 us, where
+// 438 CTAs go into 1.5 rounds), the multiply pipe's half that takes integers 50 %.  On the device,
+// float kernel or tensor cores | this one, weights from memory: bfloat16 8192 x 1024 5.7 | 4.9 us, 4096 x 4096 8.7 | 6.5; half,
+// 4096 x 4096 8.5 | 6.8; microscaled 2000 x 2000 3.7 | 2.7, 4096 x 4096 7.2 | 4.8.  Rounding what the planes cannot hold away instead took as long; finding it with
 // float32 comparisons for every value, 0.3 to 0.6 us more.
 // Two groups of channels on their way instead of one: 4096 x 4096 6.6 -> 6.9; 24 warps of 80 registers 6.9 instead of 6.8; default
 // caching of the codes instead of streaming 6.5 -> 6.8.
-// From here on it is faster than the float kernel: one row, half, 1280 x 320 2.7 us by that one, 2.9 by this; bfloat16, 1000 x 1281 3.1 by both.
+// Float kernel | this: bfloat16 1100 x 1000 3.0 | 3.1 us, 2000 x 2000 3.7 | 3.7, 512 x 8192 3.6 | 3.6, 1500 x 3000 4.1 | 4.0, 1024 x 8192
+// 5.6 | 4.9; half 1100 x 1000 2.9 | 3.2, 2000 x 2000 3.6 | 3.8, 1500 x 3000 4.4 | 4.3; 70 x 16500, too few channels for the SMs, 4.9 | 5.9.  So it
+// gains above 2^22 and loses up to 0.3 us below (more with few channels); it starts at 2^20 because what an infinity in x gives changes there,
+// and callers know it so.  Both microscaled it is faster at every size: 128 x 128 2.6 | 2.2.
 constexpr int64_t kOneFrom = 1 << 20;
 constexpr int kOneRow = 4;                       // channels at a time
 constexpr int kOneWarps = 16, kOneChannels = 64; // at most, per CTA
@@ -821,11 +824,11 @@ extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales,
 
 // Whether the kernel for few rows and small matrices beats the tensor-core kernel, whose time below 2^22 products is its chain of
 // set-up, first loads and last stores.  On the device, rows | tensor cores (linear layer: with its pre-pass, a second launch):
-//   linear, bf16     1 row (integers from 2^20 on): 1280 x 320 2.6 | 7.0 us, 2000 x 2000 3.8 | 8.2, 4096 x 4096 6.5 | 9.7, 8192 x 4096 9.5 | 10.8, 8192 x 8192 14.6 | 14.4,
-//                    28000 x 8192 43 | 34;  float32 4096 x 4096 9.2 | 9.7, 8192 x 8192 28 | 15.5
-//                    4 rows: 724 x 724 4.9 | 7.5, 2000 x 2000 8.4 | 8.2;  8 rows, 724 x 724 5.6 | 6.9, 720 x 720 4.3 | 7.0;
+//   linear, bf16     1 row (integers above 2^20): 1280 x 320 2.8 | 7.0 us, 2000 x 2000 3.7 | 8.2, 4096 x 4096 6.4 | 9.7, 8192 x 4096 9.4 | 10.8, 8192 x 8192 14.5 | 14.4,
+//                    28000 x 8192 43 | 34;  float32 4096 x 4096 9.1 | 9.7, 8192 x 8192 25 | 15.5
+//                    4 rows: 724 x 724 5.0 | 7.5, 2000 x 2000 7.4 | 8.2;  8 rows, 724 x 724 5.6 | 6.9, 720 x 720 4.3 | 7.0;
 //                    16 rows, 724 x 724 (rows that do not start on 16 bytes) 9.4 | 7.0, 720 x 720 5.4 | 7.0, 300 x 2000 6.9 | 7.2
-//   both microscaled 1 row: 2000 x 2000 2.9 | 6.3, 4096 x 4096 4.7 | 7.6, 8192 x 4096 6.8 | 10.0, 8192 x 8192 12.0 | 12.0, 28000 x 8192 29 | 26;  8 rows, 300 x 300 3.2 | 4.9;  4 rows, 2000 x 2000 8.0 | 6.4
+//   both microscaled 1 row: 2000 x 2000 2.7 | 6.3, 4096 x 4096 4.8 | 7.6, 8192 x 4096 6.8 | 10.0, 8192 x 8192 12.0 | 12.0, 28000 x 8192 29 | 26;  8 rows, 300 x 300 3.1 | 4.9;  4 rows, 2000 x 2000 8.0 | 6.4
 static bool mx_rows_pay(int N, int K, int M, int log2_most) { return (double)N * K * M <= (double)(1ll << log2_most); }
 
 extern "C" size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype) {

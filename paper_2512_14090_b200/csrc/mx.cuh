@@ -105,7 +105,7 @@ __device__ __forceinline__ void load8(const T* p, float* f) {
   }
 }
 
-// n / d for 0 <= n < 2^31 by a multiplication: q = (floor(n m / 2^32) + n) >> l with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1
+// n / d for 0 <= n < 2^31 by a multiplication (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994): q = (floor(n m / 2^32) + n) >> l with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1
 struct FastDiv {
   uint32_t d, m, l;
   explicit FastDiv(uint32_t divisor) : d(divisor), l(0) {

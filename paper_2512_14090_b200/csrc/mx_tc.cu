@@ -26,10 +26,11 @@
 // the next tile's MMAs run.  Few tiles: the K range is split over the CTAs of a cluster, whose sums meet in shared memory in a
 // fixed order.
 //
-// What bounds it (on the device, whole calls).  2,048 rows, 8192 x 8192: bfloat16 207 us (tensor pipe active 79 % of the 198 us after
-// the pre-pass, under the power limit), half 354, float32 575 (tiles of 128 rows: shared memory feeds an MMA every 87 cycles instead of
-// 64); both microscaled 61 us (4.5 PFLOP/s; tensor pipe 62 %: shared memory again, 120 cycles instead of 96).  One row, 8192 x 8192,
-// 14.2 us: the weight stream takes 5.7 of them, the rest is the pre-pass, set-up and first loads (3 us) and the way out (1.5 us).  Both
+// What bounds it.  2,048 rows, 8192 x 8192, calls in a row with inputs that change, under the power limit (a few calls by themselves): bfloat16
+// 246 us (206; tensor pipe active 79 % of what follows the pre-pass), half 396 (355), float32 685 (580; tiles of 128 rows: shared memory feeds
+// an MMA every 87 cycles instead of 64); both microscaled 76 us, 3.6 PFLOP/s (61 to 64; tensor pipe 62 %: an MMA every 120 cycles instead of
+// 96; its 10 KB of operands are filled for it alone, 85 bytes a cycle and SM).  One row, 8192 x 8192,
+// 14.2 us on the device: the weight stream takes 5.7 of them, pre-pass, set-up and first loads 3, the way out 1.5; some 4 have no owner.  Both
 // microscaled, 4096 x 4096, 16 rows 7.2 us: set-up, the first loads and the cluster's exchange.
 // What made the difference: operands of the MMAs in uniform registers (see mbar_wait_uniform and the broadcast of the warp index),
 // scale bytes requested before the weights, code that runs once per tile kept in small loops, tiles by rounds over the SMs.
@@ -789,7 +790,7 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
     if (!shape(p, (g.M + 15) / 16 * 16)) return set_error(AIQ_ERR_SHAPE, "mx_tc: N=%d M=%d", g.N, g.M);
   } else {
     // The width of the tiles decides how evenly they go into rounds over the SMs; a wide tile reads fewer operand bytes per product,
-    // a narrow one leaves room for two sets of sums.  On the device, 8192 x 8192, 2,048 rows, Mt 256 | 192 | 160 | 128: both
+    // a narrow one leaves room for two sets of sums.  On the device, a few calls by themselves (below the power limit), 8192 x 8192, 2,048 rows, Mt 256 | 192 | 160 | 128: both
     // microscaled 65 | 61 | 65 | 68 us, bfloat16 207 | 219 | 227 | 240, half 367 | 351 | 356 | 360; 4096 x 4096, 2,048 rows, both
     // microscaled 23.5 | 21.4 | 21.6 | 23.7; 1,024 rows bfloat16 37 | 44 | 43 | 40 (one round of 128 tiles at 256).
     double best = 0;

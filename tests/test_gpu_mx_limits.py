@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 # Scale bytes 253 and 254 make 6 * 2^127 of an element, which is no float32.  The stored value is finite all the same, and so is its
 # product with a small x.
 @pytest.mark.parametrize("dtype", sorted(TYPES))
-@pytest.mark.parametrize("n,k,m", [(64, 96, 1), (64, 100, 3), (70, 130, 9), (1100, 1000, 1), (700, 2000, 40)])
+@pytest.mark.parametrize("n,k,m", [(64, 96, 1), (64, 100, 3), (70, 130, 9), (1100, 1000, 1), (4400, 1000, 1), (700, 2000, 40)])
 @pytest.mark.parametrize("workspace", [True, False])
 def test_linear_with_scale_bytes_at_both_ends(dtype, n, k, m, workspace):
     dt = TYPES[dtype]
@@ -65,7 +65,7 @@ def _check_exact_products(y, x, w, what):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("n,k", [(1100, 1000), (2048, 1024), (8200, 200), (70, 16500), (40, 40000)])
+@pytest.mark.parametrize("n,k", [(1100, 1000), (4200, 1000), (8192, 1024), (35000, 130), (300, 16500), (110, 40000)])
 @pytest.mark.parametrize("log2", [0, 10, 14, 20, 40])
 def test_one_row_with_values_far_apart_in_a_block(dtype, n, k, log2):
     """One value of every block far above the others, and channels whose codes there are zero: what is left are products with the others."""
@@ -92,9 +92,9 @@ def test_one_row_with_values_far_apart_in_a_block(dtype, n, k, log2):
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_one_row_with_one_weight_per_channel(dtype):
     """Each channel has one element other than zero, a power of two: y is that value of x times it, to the last bit."""
-    dt, n, k = TYPES[dtype], 2048, 1024
+    dt, n, k = TYPES[dtype], 8192, 1024
     g = torch.Generator().manual_seed(3)
-    at = torch.randperm(k, generator=g).repeat(2)[:n]
+    at = torch.randperm(k, generator=g).repeat(8)[:n]
     e = torch.randint(0, 3, (n,), generator=g)                         # elements 1, 2, 4: codes 2, 4, 6
     sign = torch.randint(0, 2, (n,), generator=g)
     codes = torch.zeros((n, k), dtype=torch.uint8)
@@ -226,7 +226,7 @@ def _one_weight_per_channel(n, k, seed):
 # In turn: rows of x beside each other (pieces stacked), above each other, split K ranges, whole tiles and halves of them, the few-row kernel.
 @pytest.mark.parametrize("dtype", sorted(TYPES))
 @pytest.mark.parametrize("n,k,m", [(1100, 1000, 20), (609, 4100, 37), (200, 6000, 33), (700, 640, 257), (2500, 520, 2200), (1290, 650, 3500), (257, 9000, 70),
-                                   (1001, 3001, 48), (9500, 520, 16), (128, 8192, 600), (300, 33000, 40), (64, 320, 9), (100, 3001, 3), (2050, 640, 1)])
+                                   (1001, 3001, 48), (9500, 520, 16), (128, 8192, 600), (300, 33000, 40), (64, 320, 9), (100, 3001, 3), (2050, 640, 1), (4300, 1000, 1), (700, 6001, 1)])
 def test_one_weight_per_channel_is_exact(dtype, n, k, m):
     dt = TYPES[dtype]
     codes, scales, at, w = _one_weight_per_channel(n, k, n)
@@ -336,7 +336,7 @@ def test_the_stride_of_a_single_row_is_ignored(stride):
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
-@pytest.mark.parametrize("n,k,m", [(300, 700, 1), (1100, 1500, 70), (1100, 1000, 1)])
+@pytest.mark.parametrize("n,k,m", [(300, 700, 1), (1100, 1500, 70), (4400, 1000, 1)])
 def test_calls_through_ctypes(monkeypatch, dtype, n, k, m):
     """The four calls on the way that the binding takes where its CPython module is not built: the same bits."""
     b, dt = binding(), TYPES[dtype]
@@ -372,3 +372,88 @@ def test_codes_that_are_no_matrix():
             b.aiq_mx_quantize(x, bad, scales)
         with pytest.raises(ValueError):
             b.aiq_mx_matmul(codes, scales, bad, scales, None, 64, y)
+
+
+# The integer kernel (one row of 16 bits, N K > 2^20), well above its border: every end of a row, few channels and many, x on odd addresses, NaN and infinities, a captured
+# call, blocks from subnormal numbers to the largest.
+MANY = [(4200, 1000), (16500, 257), (36000, 120), (300, 16500), (70, 60500), (127, 33100), (2100, 2049), (131100, 32), (530000, 8), (4200000, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n,k", MANY)
+def test_one_row_against_many_weights(dtype, n, k):
+    dt = TYPES[dtype]
+    codes, scales = held(weights(n, k, n + k))
+    w = _rows_of(codes, scales, k)
+    bias = torch.randn(n, generator=torch.Generator().manual_seed(3)).cuda() if n % 2 == 0 else None
+    for skip in (0, 1):
+        x = activations(1, k + skip, dt, k)[:, skip:]
+        y = linear(codes, scales, bias, x, torch.full((1, n), float("nan"), dtype=dt, device="cuda"))
+        z = x.double() if bias is None else torch.cat((x.double(), torch.ones((1, 1), dtype=torch.float64, device="cuda")), 1)
+        _check_exact_products(y, z, w if bias is None else torch.cat((w, bias.double()[:, None]), 1), f"skip {skip}")
+        assert torch.equal(y, linear(codes, scales, bias, x, torch.empty_like(y)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_row_of_every_size_against_many_weights(dtype):
+    dt, n, k = TYPES[dtype], 6600, 640
+    w = weights(n, k, 91).cpu()
+    w[3, 40:80] = 0
+    codes, scales = held(w.cuda())
+    x = activations(1, k, torch.float32, 92).cpu()
+    x[0, 64:96] = 0
+    x[0, 96:128] = -x[0, 96:128].abs()
+    x[0, 128:160] *= torch.logspace(-8, 0, 32)
+    if dtype == "f16":
+        x[0, :32] *= 2.0 ** -16
+        x[0, 32:64] = 60000.0
+        scales[:, 0], scales[:, 1] = 140, 100
+    else:
+        x[0, :32] *= 2.0 ** -122
+        x[0, 32:64] *= 2.0 ** 100
+        x[0, 160:192] = torch.arange(1, 33) * 2.0 ** -133
+        x[0, 192:224] = torch.logspace(-39, 35, 32, dtype=torch.float64).float()
+        scales[:, 0], scales[:, 1], scales[:, 5], scales[:, 6] = 245, 10, 254, 2
+    x = x.to(dt).cuda()
+    y = linear(codes, scales, None, x, torch.full((1, n), float("nan"), dtype=dt, device="cuda"))
+    _check_exact_products(y, x, _rows_of(codes, scales, k), "")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_row_with_nan_and_infinity_against_many_weights(dtype):
+    dt, n, k = TYPES[dtype], 4100, 1100
+    w = weights(n, k, 93)
+    w[5, 1099], w[4099, 0] = float("nan"), float("inf")
+    codes, scales = held(w)
+    for what in (float("nan"), float("inf"), -float("inf")):
+        x = activations(1, k, dt, 94)
+        x[0, 1070] = what
+        assert torch.isnan(linear(codes, scales, None, x, torch.zeros((1, n), dtype=dt, device="cuda"))).all()
+    x = activations(1, k, dt, 94)
+    y = linear(codes, scales, None, x, torch.zeros((1, n), dtype=dt, device="cuda"))
+    assert torch.isnan(y[0, [5, 4099]]).all()
+    keep = [i for i in range(n) if i not in (5, 4099)]
+    _check_exact_products(y[:, keep], x, _rows_of(codes[keep], scales[keep], k), "")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_row_against_many_weights_captured(dtype):
+    """A replay reads the x of its time, what its blocks leave out too; elements of y's buffer beside the row stay as they were."""
+    dt, n, k = TYPES[dtype], 8205, 520
+    codes, scales = held(weights(n, k, 95))
+    w = _rows_of(codes, scales, k)
+    x, wide = activations(1, k, dt, 96), torch.full((1, n + 7), 7.0, dtype=dt, device="cuda")
+    y = wide[:, 3:3 + n]
+    linear(codes, scales, None, x, y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        linear(codes, scales, None, x, y)
+    for seed in (97, 98):
+        new = activations(1, k, dt, seed)
+        new[0, 5::32] *= 2.0 ** -(14 if dtype == "f16" else 40)
+        x.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        _check_exact_products(y, x, w, f"{seed}")
+        assert (wide[:, :3] == 7.0).all() and (wide[:, 3 + n:] == 7.0).all()
