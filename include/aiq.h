@@ -190,23 +190,24 @@ aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales, int rows, 
 /* The linear layer with microscaled weights:  y[m][n] = sum_k x[m][k] W[n][k] + bias[n],  W [N][K] as codes and scales,
  * x [M][K] and y [M][N] of `dtype`, bias float32 [N] or NULL.  Sums are float32; run-to-run identical.
  *
- * Three kernels.  Two need no workspace, and every product of theirs is exact: one for few rows and small matrices multiplies in
- * float32, one for a single row of 16-bit values (N K > 2^20) in integers, with what those leave out of x in float32.  The third, for the rest, runs on
- * the tensor cores' block-scaled MMAs (tcgen05, kind::mxf8f6f4): a pre-pass writes x into `workspace` as a sum of eight-bit
- * floats, 2 for bfloat16, 3 for half, 5 for float32, with a scale for every 32 values.  They hold x exactly, save what lies
- * below 2^-22 (bfloat16), 2^-27 (half), 2^-37 (float32) of the largest of the 32 values; their products are exact.  (What that costs where one of
- * 32 activations is r times the others and a channel's weight there is zero: bfloat16 1e-2 of such a channel's y at r = 1e5, float32 3e-6 at 1e6,
- * nothing beside the rounding of y at 1e3.)  The MMAs cut a sum where
- * float32 would round it, which costs a 16-bit result up to a tenth of its own rounding; sums that would lose more, and those of float32 results,
- * are added up in float32 every 512 k.  In the last two kernels a block
- * with an infinity or a NaN makes its row of y NaN; in float32 an infinity gives what IEEE arithmetic does.  Which kernel runs depends on the
- * sizes, so a row's last bits depend on how many rows come with it.  `workspace`: device, 16-byte aligned,
- * aiq_mx_linear_workspace_bytes(...) bytes (0 where one of the first
- * two is chosen or an argument is out of range), not used by two calls at a time.  NULL: the first two, whatever the size, which makes every
- * product exact and takes long where the third would have been chosen: 8192 x 8192, bfloat16, 64 rows 0.85 ms instead of 0.021, 2,048 rows 32 ms
- * instead of 0.25.
- * The waits of the tensor-core kernel for copies, scales and sums are bounded (about 2 s); should one run out, that block's part of y becomes NaN.
- * (Tensor memory, and the other blocks of a cluster, are waited for as long as it takes the kernels that hold the one and the others to end.) */
+ * Three kernels.  Two need no workspace, and every product of theirs is exact: one for few rows and small matrices multiplies
+ * in float32, one for a single row of 16-bit values (N K > 2^20) in integers, with what those leave out of x in float32.  The
+ * third, for the rest, runs on the tensor cores' block-scaled MMAs (tcgen05, kind::mxf8f6f4): a pre-pass writes x into
+ * `workspace` as a sum of eight-bit floats, 2 for bfloat16, 3 for half, 5 for float32, with a scale for every 32 values.  They
+ * hold x exactly, save what lies below 2^-22 (bfloat16), 2^-27 (half), 2^-37 (float32) of the largest of the 32 values; their
+ * products are exact.  (What that costs where one of 32 activations is r times the others and a channel's weight there is zero:
+ * bfloat16 1e-2 of such a channel's y at r = 1e5, float32 3e-6 at 1e6, nothing beside the rounding of y at 1e3.) The MMAs cut a
+ * sum where float32 would round it, which costs a 16-bit result up to a tenth of its own rounding; sums that would lose more,
+ * and those of float32 results, are added up in float32 every 512 k.  In the last two kernels a block with an infinity or a NaN
+ * makes its row of y NaN; in the first an infinity gives what IEEE arithmetic does.  Which kernel runs depends on the sizes, so
+ * a row's last bits depend on how many rows come with it.  `workspace`: device, 16-byte aligned,
+ * aiq_mx_linear_workspace_bytes(...) bytes (0 where one of the first two is chosen or an argument is out of range), not used by
+ * two calls at a time.
+ * NULL: the first two, whatever the size, which makes every product exact and takes long where the third would have been
+ * chosen: 8192 x 8192, bfloat16, 64 rows 0.85 ms instead of 0.021, 2,048 rows 32 ms instead of 0.25.
+ * The waits of the tensor-core kernel for copies, scales and sums are bounded (about 2 s); should one run out, that block's
+ * part of y becomes NaN.  (Tensor memory, and the other blocks of a cluster, are waited for as long as it takes the kernels
+ * that hold the one and the others to end.) */
 size_t aiq_mx_linear_workspace_bytes(int N, int K, int M, int dtype);
 aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
                            int M, int64_t x_stride, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,

@@ -822,6 +822,7 @@ extern "C" aiq_status_t aiq_mx_dequantize(const void* codes, const void* scales,
                                    (cudaStream_t)stream);
 }
 
+// (Rows of x that do not start on 16 bytes are told by K: their stride and address are not known when the workspace is asked for.)
 // Whether the kernel for few rows and small matrices beats the tensor-core kernel, whose time below 2^22 products is its chain of
 // set-up, first loads and last stores.  On the device, rows | tensor cores (linear layer: with its pre-pass, a second launch):
 //   linear, bf16     1 row (integers above 2^20): 1280 x 320 2.8 | 7.0 us, 2000 x 2000 3.7 | 8.2, 4096 x 4096 6.4 | 9.7, 8192 x 4096 9.4 | 10.8, 8192 x 8192 14.5 | 14.4,
