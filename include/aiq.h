@@ -13,6 +13,9 @@
  *   aiq_qlinear          y = x * dequant(W)^T for a packed weight matrix (small batch)
  *   aiq_mx_quantize, aiq_mx_dequantize, aiq_mx_linear, aiq_mx_matmul
  *                        microscaled 4-bit floating point: a scale for every 32 values instead of one per channel
+ *   aiq_mx_linear_act    the same linear layer with an activation, a gate and a residual
+ *   aiq_route_experts, aiq_plan_experts, aiq_mx_linear_experts, aiq_combine_experts
+ *                        a layer of experts with microscaled weights
  *   aiq_model_create     fold, then build the L x {4,8,16,32} bank of packed weights
  *   aiq_forward          logits of one scheme on one image batch
  *   aiq_eval_schemes     top-1 agreement of many schemes on an image set
@@ -217,7 +220,73 @@ aiq_status_t aiq_mx_linear(const void* codes, const void* scales, const float* b
  * kind::mxf4 on the tensor cores, which take codes and scales as they are stored; the kernels for small matrices and for a single row as above. */
 aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales, int M, const void* b_codes, const void* b_scales, int N,
                            const float* bias, int K, void* y, int dtype, int64_t y_stride, void* stream);
-/* Test aid for what happens when a wait runs out, beside aiq_debug_expire_wait: the next aiq_mx_linear or aiq_mx_matmul of the calling thread that
+/* The linear layer with what usually follows it, in one pass over y:
+ *     gated = 0:  y[m][n] = act(sum_k x[m][k] W[n][k] + bias[n]) + residual[m][n],                      n < N
+ *     gated = 1:  y[m][n] = act(sum_k x[m][k] W[n][k] + bias[n]) * (sum_k x[m][k] W[N/2 + n][k] + bias[N/2 + n]) + residual[m][n],
+ *                 n < N / 2: the first half of the rows of W are the gates, the second what they multiply (N even)
+ * in float32, rounded once.  activation: AIQ_ACT_NONE, _RELU, _RELU6 (see the model description), SILU v / (1 + exp(-v)), GELU v Phi(v) with the
+ * normal distribution's Phi, or GELU_TANH, its approximation v / (1 + exp(-2 sqrt(2/pi) (v + 0.044715 v^3))); a NaN stays one.
+ * residual: rows of `dtype`, stride r_stride (ignored for a single row), or NULL; it may be y itself.  The rest as aiq_mx_linear: the
+ * three kernels, the same workspace size, workspace NULL. */
+enum { AIQ_ACT_SILU = 3, AIQ_ACT_GELU = 4, AIQ_ACT_GELU_TANH = 5 };
+aiq_status_t aiq_mx_linear_act(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
+                               int M, int64_t x_stride, int activation, int gated, const void* residual, int64_t r_stride,
+                               void* y, int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Experts.  A layer of E experts (1 to 1024), each with microscaled weights of its own, of which every token uses up to top_k (1 to 31, at most E):
+ *     aiq_route_experts       which experts, and their weights; with a plan
+ *     aiq_plan_experts        the plan alone, of given experts
+ *     aiq_mx_linear_experts   the experts' linear layers, for all tokens
+ *     aiq_combine_experts     a token's sum of what its experts gave
+ * T tokens, T top_k at most 2^30; asynchronous on `stream`, may be captured, run-to-run identical.
+ *
+ * A plan sorts the (token, place) pairs by expert, and by token within an expert: pair t top_k + j is place j of token t.  It is int32 words in
+ * device memory, 16-byte aligned, aiq_expert_plan_bytes(...) bytes (0 for sizes out of range), of which these parts may be read
+ * (aiq_expert_plan_parts: where they start, in bytes):
+ *     offsets [E + 1]        the first row of each expert, and the number of rows
+ *     slots [T top_k]        the pair of each row; -1 behind the last
+ *     positions [T top_k]    the row of each pair; -1 for one without an expert
+ * It serves calls of the same T, top_k and E.  (A call given another one, or memory that holds none, leaves y as it is, or NaN in
+ * aiq_combine_experts.) */
+size_t aiq_expert_plan_bytes(int T, int top_k, int E);
+aiq_status_t aiq_expert_plan_parts(int T, int top_k, int E, size_t* offsets, size_t* slots, size_t* positions);
+/* ids: device int32 [T][top_k]; what is not in 0 .. E - 1 is no expert. */
+aiq_status_t aiq_plan_experts(const int32_t* ids, int T, int top_k, int E, void* plan, size_t plan_bytes, void* stream);
+
+/* logits [T][E] of `dtype`, rows `stride` elements apart (ignored for a single row); bias float32 [E] or NULL.
+ *   score p[e]   softmax over the token's logits, or 1 / (1 + exp(-logit))
+ *   choice       p[e] + bias[e]
+ *   groups       the E experts are `groups` (1 to 32) runs of E / groups; a group counts as much as the best choice in it (group_best = 1) or the sum of the two best
+ *                (2; of the one, where it has one); only experts of the top_groups first groups are chosen
+ *   ids          the top_k largest choices, in order; of equal ones (of groups, too) the lower index
+ *   weights      p[ids] scale, or renormalise = 1: p[ids] / (sum of these) scale
+ * An expert whose logit or bias is -infinity is not chosen, and a group of such not either; where fewer than top_k are left ids are -1 and weights 0.  Choices, and sums of two, are
+ * told apart as in float64; single ones without a bias as the logits, whose order they have.  Weights are float32.  A token with a NaN among logits or bias, or with a
+ * logit of +infinity under softmax, gets ids of -1 and weights of NaN.
+ * ids int32 [T][top_k], weights float32 [T][top_k]; plan: filled as by aiq_plan_experts, or NULL. */
+enum { AIQ_SCORE_SOFTMAX = 0, AIQ_SCORE_SIGMOID = 1 };
+aiq_status_t aiq_route_experts(const void* logits, int dtype, int T, int E, int64_t stride, const float* bias, int scoring, int top_k,
+                               int groups, int top_groups, int group_best, int renormalise, float scale, int32_t* ids, float* weights,
+                               void* plan, size_t plan_bytes, void* stream);
+
+/* y[row] = what aiq_mx_linear_act gives without a residual, with W and bias of the row's expert, for every row of the plan; the other rows of y
+ * stay as they are.  codes, scales: [E][N] rows as above, bias float32 [E][N] or NULL, y [T top_k][N, gated: N / 2].
+ * x_sorted = 0: x [T][K], a row per token; 1: x [T top_k][K] in the plan's rows (what an earlier call wrote).  x and y may not overlap.
+ * On the tensor cores for every size, as the third kernel of aiq_mx_linear (precision, bounded waits); weights of experts without rows are not read.
+ * workspace: device, 16-byte aligned, aiq_mx_linear_experts_workspace_bytes(E, N, K, T top_k, dtype) bytes, not used by two calls at a time. */
+size_t aiq_mx_linear_experts_workspace_bytes(int E, int N, int K, int rows, int dtype);
+aiq_status_t aiq_mx_linear_experts(const void* codes, const void* scales, const float* bias, int E, int N, int K, const void* x, int dtype,
+                                   int64_t x_stride, int x_sorted, const void* plan, size_t plan_bytes, int T, int top_k, int activation,
+                                   int gated, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* y[t] = residual[t] + sum_j weights[t][j] z[positions[t][j]]: z [T top_k][H] in the plan's rows, y and residual (or NULL; it may be y itself) [T][H], of `dtype`; weights
+ * float32 [T][top_k].  Summed in float32 in the order of j, rounded once.  A pair without an expert adds its weight times zero, so that a
+ * NaN among the weights shows. */
+aiq_status_t aiq_combine_experts(const void* z, int dtype, int T, int top_k, int E, int H, int64_t z_stride, const float* weights,
+                                 const void* plan, size_t plan_bytes, const void* residual, int64_t r_stride, void* y, int64_t y_stride,
+                                 void* stream);
+
+/* Test aid for what happens when a wait runs out, beside aiq_debug_expire_wait: the next aiq_mx_linear, aiq_mx_matmul, aiq_mx_linear_act or aiq_mx_linear_experts of the calling thread that
  * runs on the tensor cores holds one kind of arrival back and gives its waits up after `limit_cycles` SM clocks (at most 2e9; 0: takes the
  * request back).  It ends in an ordinary way, with NaN in all of y. */
 aiq_status_t aiq_debug_mx_expire_wait(int64_t limit_cycles);

@@ -17,7 +17,8 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED_BITS, ERR_SHAPE, ERR_WORKSPACE_TOO_SMALL = 1, 2
 ERR_CUDA, ERR_NOT_SM100, ERR_NONFINITE, ERR_TIMEOUT = 5, 6, 7, 8
 
 LAYER_KIND = {"conv": 0, "dw": 1, "fc": 2}
-ACT = {"none": 0, "relu": 1, "relu6": 2}
+ACT = {"none": 0, "relu": 1, "relu6": 2, "silu": 3, "gelu": 4, "gelu_tanh": 5}        # a model's layers take the first three
+SCORE = {"softmax": 0, "sigmoid": 1}
 
 EXPORTS = [
     "aiq_status_string", "aiq_last_error", "aiq_fold_bn", "aiq_packed_row_bytes",
@@ -27,7 +28,9 @@ EXPORTS = [
     "aiq_eval_schemes", "aiq_set_eval_options", "aiq_set_fusion", "aiq_set_small_pass_images", "aiq_quantize_layer_per_tensor", "aiq_set_scale_granularity", "aiq_last_call_stats", "aiq_scheme_ai",
     "aiq_profile_start", "aiq_profile_stop", "aiq_forward_static",
     "aiq_mx_row_bytes", "aiq_mx_scale_row_bytes", "aiq_mx_quantize", "aiq_mx_dequantize", "aiq_mx_linear_workspace_bytes",
-    "aiq_mx_linear", "aiq_mx_matmul", "aiq_debug_mx_expire_wait",
+    "aiq_mx_linear", "aiq_mx_matmul", "aiq_debug_mx_expire_wait", "aiq_mx_linear_act",
+    "aiq_expert_plan_bytes", "aiq_expert_plan_parts", "aiq_plan_experts", "aiq_route_experts", "aiq_mx_linear_experts_workspace_bytes",
+    "aiq_mx_linear_experts", "aiq_combine_experts",
     "aiq_set_compute_path", "aiq_model_status", "aiq_debug_expire_wait", "aiq_search_greedy", "aiq_search_coordinate_descent",
 ]
 
@@ -109,6 +112,22 @@ def _load():
     lib.aiq_mx_linear_workspace_bytes.argtypes = [n32, n32, n32, n32]
     lib.aiq_mx_linear.restype = i32
     lib.aiq_mx_linear.argtypes = [vp, vp, vp, n32, n32, vp, n32, n32, i64, vp, i64, vp, sz, vp]
+    lib.aiq_mx_linear_act.restype = i32
+    lib.aiq_mx_linear_act.argtypes = [vp, vp, vp, n32, n32, vp, n32, n32, i64, n32, n32, vp, i64, vp, i64, vp, sz, vp]
+    lib.aiq_expert_plan_bytes.restype = sz
+    lib.aiq_expert_plan_bytes.argtypes = [n32, n32, n32]
+    lib.aiq_expert_plan_parts.restype = i32
+    lib.aiq_expert_plan_parts.argtypes = [n32, n32, n32, C.POINTER(sz), C.POINTER(sz), C.POINTER(sz)]
+    lib.aiq_plan_experts.restype = i32
+    lib.aiq_plan_experts.argtypes = [vp, n32, n32, n32, vp, sz, vp]
+    lib.aiq_route_experts.restype = i32
+    lib.aiq_route_experts.argtypes = [vp, n32, n32, n32, i64, vp, n32, n32, n32, n32, n32, n32, f32, vp, vp, vp, sz, vp]
+    lib.aiq_mx_linear_experts_workspace_bytes.restype = sz
+    lib.aiq_mx_linear_experts_workspace_bytes.argtypes = [n32, n32, n32, n32, n32]
+    lib.aiq_mx_linear_experts.restype = i32
+    lib.aiq_mx_linear_experts.argtypes = [vp, vp, vp, n32, n32, n32, vp, n32, i64, n32, vp, sz, n32, n32, n32, n32, vp, i64, vp, sz, vp]
+    lib.aiq_combine_experts.restype = i32
+    lib.aiq_combine_experts.argtypes = [vp, n32, n32, n32, n32, n32, i64, vp, vp, sz, vp, i64, vp, i64, vp]
     lib.aiq_debug_mx_expire_wait.restype = i32
     lib.aiq_debug_mx_expire_wait.argtypes = [i64]
     lib.aiq_mx_matmul.restype = i32
@@ -364,6 +383,120 @@ def _mx_check_matmul(a_codes, a_scales, b_codes, b_scales, bias, y, K):
     return m, n, dtype, y_stride
 
 
+def _choice(names, name, what):
+    code = names.get(name)
+    if code is None:
+        raise ValueError(f"expected one of {', '.join(names)} as {what}, not {name!r}")
+    return code
+
+
+def _mx_outputs(n, gated):
+    if gated and n % 2:
+        raise ValueError(f"gated, but weights of {n} rows")
+    return n // 2 if gated else n
+
+
+def _mx_check_linear_act(codes, scales, bias, x, y, activation, gated, residual):
+    act = _choice(ACT, activation, "activation")
+    dtype, m, k, x_stride = _mx_rows(x)
+    y_dtype, y_rows, outputs, y_stride = _mx_rows(y)
+    n = _mx_held(codes, scales, k)
+    if (y_dtype, y_rows, outputs) != (dtype, m, _mx_outputs(n, gated)):
+        raise ValueError(f"x {tuple(x.shape)} {x.dtype}, weights of {n} rows and y {tuple(y.shape)} {y.dtype} do not match")
+    _mx_bias(bias, n)
+    r_stride = 0
+    if residual is not None:
+        r_dtype, r_rows, r_width, r_stride = _mx_rows(residual)
+        if (r_dtype, r_rows, r_width) != (dtype, m, outputs):
+            raise ValueError(f"residual {tuple(residual.shape)} {residual.dtype} and y {tuple(y.shape)} {y.dtype} do not match")
+    return n, k, dtype, m, x_stride, act, int(bool(gated)), r_stride, y_stride
+
+
+def _expert_array(t, dtype, shape, what):
+    if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"expected {what} as a contiguous {dtype} {shape}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _expert_plan(plan, T, top_k, E):
+    """Bytes of a plan that is large enough."""
+    needed = int(lib.aiq_expert_plan_bytes(T, top_k, E))
+    if needed == 0:
+        _check(lib.aiq_expert_plan_parts(T, top_k, E, None, None, None))
+    size = plan.numel() * plan.element_size()
+    if not plan.is_contiguous() or size < needed:
+        raise ValueError(f"expected a contiguous plan of {needed} bytes for {T} tokens, {top_k} of {E} experts, not {size}")
+    return size
+
+
+def _check_route(logits, ids, weights, bias, scoring, plan):
+    import torch
+    dtype, t, e, stride = _mx_rows(logits)
+    if ids.dim() != 2:
+        raise ValueError(f"expected ids of a row per token, not {tuple(ids.shape)}")
+    top_k = ids.shape[1]
+    _expert_array(ids, torch.int32, (t, top_k), "ids")
+    _expert_array(weights, torch.float32, (t, top_k), "weights")
+    _mx_bias(bias, e)
+    return dtype, t, e, stride, _choice(SCORE, scoring, "scoring"), top_k, 0 if plan is None else _expert_plan(plan, t, top_k, e)
+
+
+def _check_plan(ids, plan, e):
+    import torch
+    if ids.dim() != 2:
+        raise ValueError(f"expected ids of a row per token, not {tuple(ids.shape)}")
+    t, top_k = ids.shape
+    _expert_array(ids, torch.int32, (t, top_k), "ids")
+    return t, top_k, _expert_plan(plan, t, top_k, e)
+
+
+def _check_experts(codes, scales, bias, x, plan, top_k, y, activation, gated, x_sorted):
+    act = _choice(ACT, activation, "activation")
+    dtype, x_rows, k, x_stride = _mx_rows(x)
+    y_dtype, rows, outputs, y_stride = _mx_rows(y)
+    if codes.dim() != 3 or scales.dim() != 3:
+        raise ValueError(f"expected codes and scales of a matrix per expert, not {tuple(codes.shape)} and {tuple(scales.shape)}")
+    e, n = codes.shape[:2]
+    if scales.shape[0] != e or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("expected contiguous codes and scales of as many experts")
+    _mx_held(codes.reshape(e * n, codes.shape[2]), scales.reshape(e * scales.shape[1], scales.shape[2]), k)
+    t = rows // top_k if top_k > 0 else 0
+    if (y_dtype, t * top_k, outputs) != (dtype, rows, _mx_outputs(n, gated)) or x_rows != (rows if x_sorted else t):
+        raise ValueError(f"x {tuple(x.shape)} {x.dtype}, {top_k} of {e} experts of {n} rows and y {tuple(y.shape)} {y.dtype} do not match")
+    if bias is not None and tuple(bias.shape) != (e, n):
+        raise ValueError(f"expected a bias of {(e, n)}, not {tuple(bias.shape)}")
+    _mx_bias(bias, e * n)
+    return e, n, k, dtype, x_stride, int(bool(x_sorted)), _expert_plan(plan, t, top_k, e), t, act, int(bool(gated)), y_stride
+
+
+def _check_combine(z, weights, plan, e, y, residual):
+    import torch
+    dtype, rows, width, z_stride = _mx_rows(z)
+    if weights.dim() != 2:
+        raise ValueError(f"expected weights of a row per token, not {tuple(weights.shape)}")
+    t, top_k = weights.shape
+    _expert_array(weights, torch.float32, (t, top_k), "weights")
+    r_stride = 0
+    for what, m, of in (("z", z, t * top_k), ("y", y, t), ("residual", residual, t)):
+        if m is not None:
+            m_dtype, m_rows, m_width, stride = _mx_rows(m)
+            if (m_dtype, m_rows, m_width) != (dtype, of, width):
+                raise ValueError(f"{what} {tuple(m.shape)} {m.dtype}, z {tuple(z.shape)} {z.dtype} and weights {(t, top_k)} do not match")
+            if what == "y":
+                y_stride = stride
+            elif what == "residual":
+                r_stride = stride
+    return dtype, t, top_k, width, z_stride, _expert_plan(plan, t, top_k, e), r_stride, y_stride
+
+
+def _bytes(t):
+    """What a check of a tensor without strides looks at."""
+    return (t.shape, t.dtype, t.is_contiguous()) if t is not None else None
+
+
+def _matrix(t):
+    return (t.shape, t.stride(), t.dtype) if t is not None else None
+
+
 def aiq_mx_row_bytes(K):
     return int(lib.aiq_mx_row_bytes(int(K)))
 
@@ -427,6 +560,106 @@ def aiq_mx_matmul(a_codes, a_scales, b_codes, b_scales, bias, K, y, stream=None)
                    and (bias is None or bias.get_device() == d))
     status = _mxcall.aiq_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), m, b_codes.data_ptr(), b_scales.data_ptr(), n,
                                bias.data_ptr() if bias is not None else None, int(K), y.data_ptr(), dtype, y_stride, s)
+    if status:
+        _check(status)
+
+
+def aiq_mx_linear_act(codes, scales, bias, x, y, activation="none", gated=False, residual=None, workspace=None, stream=None):
+    """y [M][N] = act(x W^T + bias) + residual; gated: y [M][N / 2] = act(x G^T + bias_g) * (x U^T + bias_u) + residual, G and U the first and the second
+    half of the rows of W.  activation: "none", "relu", "relu6", "silu", "gelu" or "gelu_tanh"; residual as y, which it may be.  The rest as
+    aiq_mx_linear, the workspace's size too."""
+    key = ("act", activation, gated, _bytes(codes), _bytes(scales), _bytes(bias), _matrix(x), _matrix(y), _matrix(residual))
+    n, k, dtype, m, x_stride, act, gate, r_stride, y_stride = (
+        _mx_plans.get(key) or _mx_plan(key, _mx_check_linear_act, codes, scales, bias, x, y, activation, gated, residual))
+    d = x.get_device()
+    s = _mx_stream(stream, d, d == y.get_device() == codes.get_device() == scales.get_device()
+                   and (bias is None or bias.get_device() == d) and (residual is None or residual.get_device() == d)
+                   and (workspace is None or workspace.get_device() == d))
+    ws, size = (_dev(workspace), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
+    status = _mxcall.aiq_mx_linear_act(codes.data_ptr(), scales.data_ptr(), bias.data_ptr() if bias is not None else None, n, k, x.data_ptr(), dtype, m,
+                                       x_stride, act, gate, residual.data_ptr() if residual is not None else None, r_stride, y.data_ptr(), y_stride,
+                                       ws, size, s)
+    if status:
+        _check(status)
+
+
+# ------------------------------------------------------------------------------- experts
+def aiq_expert_plan_bytes(T, top_k, E):
+    return int(lib.aiq_expert_plan_bytes(int(T), int(top_k), int(E)))
+
+
+def aiq_expert_plan_parts(plan, T, top_k, E):
+    """Views of a plan's int32 parts: offsets [E + 1], slots [T * top_k], positions [T][top_k]."""
+    key = ("parts", T, top_k, E)
+    at = _mx_plans.get(key)
+    if at is None:
+        starts = [C.c_size_t() for _ in range(3)]
+        _check(lib.aiq_expert_plan_parts(T, top_k, E, *[C.byref(a) for a in starts]))
+        at = _mx_plans[key] = [a.value // 4 for a in starts]
+    import torch
+    w = plan.view(torch.int32)
+    return w[at[0]:at[0] + E + 1], w[at[1]:at[1] + T * top_k], w[at[2]:at[2] + T * top_k].view(T, top_k)
+
+
+def aiq_plan_experts(ids, E, plan, stream=None):
+    """ids int32 [T][top_k] -> plan, a tensor of aiq_expert_plan_bytes(T, top_k, E) bytes."""
+    key = ("plan", E, _bytes(ids), _bytes(plan))
+    t, top_k, size = _mx_plans.get(key) or _mx_plan(key, _check_plan, ids, plan, int(E))
+    d = ids.get_device()
+    s = _mx_stream(stream, d, d == plan.get_device())
+    status = _mxcall.aiq_plan_experts(ids.data_ptr(), t, top_k, int(E), plan.data_ptr(), size, s)
+    if status:
+        _check(status)
+
+
+def aiq_route_experts(logits, ids, weights, bias=None, scoring="softmax", groups=1, top_groups=1, group_best=1, renormalise=True, scale=1.0, plan=None,
+                      stream=None):
+    """logits [T][E] float32, float16 or bfloat16 -> ids int32 [T][top_k], weights float32 [T][top_k] and, where given, a plan of
+    aiq_expert_plan_bytes(T, top_k, E) bytes.  scoring: "softmax" or "sigmoid"; bias float32 [E] or None."""
+    key = ("route", scoring, _matrix(logits), _bytes(ids), _bytes(weights), _bytes(bias), _bytes(plan))
+    dtype, t, e, stride, score, top_k, size = _mx_plans.get(key) or _mx_plan(key, _check_route, logits, ids, weights, bias, scoring, plan)
+    d = logits.get_device()
+    s = _mx_stream(stream, d, d == ids.get_device() == weights.get_device() and (bias is None or bias.get_device() == d)
+                   and (plan is None or plan.get_device() == d))
+    status = _mxcall.aiq_route_experts(logits.data_ptr(), dtype, t, e, stride, bias.data_ptr() if bias is not None else None, score, top_k,
+                                       int(groups), int(top_groups), int(group_best), int(bool(renormalise)), float(scale), ids.data_ptr(),
+                                       weights.data_ptr(), plan.data_ptr() if plan is not None else None, size, s)
+    if status:
+        _check(status)
+
+
+def aiq_mx_linear_experts_workspace_bytes(E, N, K, rows, dtype):
+    return int(lib.aiq_mx_linear_experts_workspace_bytes(int(E), int(N), int(K), int(rows), _dtype(dtype)))
+
+
+def aiq_mx_linear_experts(codes, scales, bias, x, plan, top_k, y, activation="none", gated=False, x_sorted=False, workspace=None, stream=None):
+    """y [T * top_k][N, gated: N / 2] = act(x W^T + bias) for the plan's rows, with each row's expert's weights: codes [E][N][aiq_mx_row_bytes(K)], scales
+    [E][N][aiq_mx_scale_row_bytes(K)], bias float32 [E][N] or None.  x [T][K], or [T * top_k][K] in the plan's rows (x_sorted).  workspace: a tensor of
+    aiq_mx_linear_experts_workspace_bytes(E, N, K, T * top_k, x.dtype) bytes."""
+    key = ("experts", activation, gated, x_sorted, top_k, _bytes(codes), _bytes(scales), _bytes(bias), _matrix(x), _matrix(y), _bytes(plan))
+    e, n, k, dtype, x_stride, in_order, size, t, act, gate, y_stride = (
+        _mx_plans.get(key) or _mx_plan(key, _check_experts, codes, scales, bias, x, plan, int(top_k), y, activation, gated, x_sorted))
+    if workspace is None:
+        raise ValueError("expected a workspace")
+    d = x.get_device()
+    s = _mx_stream(stream, d, d == y.get_device() == codes.get_device() == scales.get_device() == plan.get_device() == workspace.get_device()
+                   and (bias is None or bias.get_device() == d))
+    status = _mxcall.aiq_mx_linear_experts(codes.data_ptr(), scales.data_ptr(), bias.data_ptr() if bias is not None else None, e, n, k, x.data_ptr(), dtype,
+                                           x_stride, in_order, plan.data_ptr(), size, t, int(top_k), act, gate, y.data_ptr(), y_stride,
+                                           _dev(workspace), workspace.numel() * workspace.element_size(), s)
+    if status:
+        _check(status)
+
+
+def aiq_combine_experts(z, weights, plan, E, y, residual=None, stream=None):
+    """y [T][H] = residual + the weighted sum of each token's rows of z [T * top_k][H]; weights float32 [T][top_k]; residual as y, which it may be."""
+    key = ("combine", E, _matrix(z), _bytes(weights), _bytes(plan), _matrix(y), _matrix(residual))
+    dtype, t, top_k, width, z_stride, size, r_stride, y_stride = (
+        _mx_plans.get(key) or _mx_plan(key, _check_combine, z, weights, plan, int(E), y, residual))
+    d = z.get_device()
+    s = _mx_stream(stream, d, d == weights.get_device() == plan.get_device() == y.get_device() and (residual is None or residual.get_device() == d))
+    status = _mxcall.aiq_combine_experts(z.data_ptr(), dtype, t, top_k, int(E), width, z_stride, weights.data_ptr(), plan.data_ptr(), size,
+                                         residual.data_ptr() if residual is not None else None, r_stride, y.data_ptr(), y_stride, s)
     if status:
         _check(status)
 

@@ -320,10 +320,20 @@ struct RowsHeld {
   }
 };
 
-template <typename X, typename T, int MT, int U>
+// FUSED: an activation, a gate and a residual on the way out.  With a gate, channel n of a warp is row n / 2 of the weights' first half (n even) or
+// second half (n odd), so that a gate and its factor are in the same warp.
+struct MxTail {
+  int act, gated;
+  const void* residual;
+  int64_t r_stride;
+};
+template <bool FUSED>
+__device__ __forceinline__ int weight_row(const MxTail& tail, int n, int N) { return FUSED && tail.gated ? (n & 1) * (N >> 1) + (n >> 1) : n; }
+
+template <typename X, typename T, int MT, int U, bool FUSED>
 __global__ void __launch_bounds__(kMxThreads)
 mx_product_rows_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t row_bytes, int64_t scale_row,
-                       const float* __restrict__ bias, int N, int K, int M, int k_warps, T* __restrict__ y, int64_t y_stride) {
+                       const float* __restrict__ bias, int N, int K, int M, int k_warps, T* __restrict__ y, int64_t y_stride, MxTail tail) {
   constexpr int R = kRowChannels, WARPS = kMxThreads / 32;
   __shared__ float part[WARPS][R * MT];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kw = warp % k_warps;
@@ -344,8 +354,9 @@ mx_product_rows_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __
 #pragma unroll
         for (int i = 0; i < R; ++i) {
           const bool live = w < words && n0 + i < N;
-          raw[i][u] = live ? *reinterpret_cast<const uint32_t*>(codes + (n0 + i) * row_bytes + (int64_t)w * 4) : 0u;
-          sb[i][u] = live ? scales[(n0 + i) * scale_row + (w >> 2)] : 0u;
+          const int64_t row = weight_row<FUSED>(tail, n0 + i, N);
+          raw[i][u] = live ? *reinterpret_cast<const uint32_t*>(codes + row * row_bytes + (int64_t)w * 4) : 0u;
+          sb[i][u] = live ? scales[row * scale_row + (w >> 2)] : 0u;
         }
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
@@ -392,13 +403,30 @@ mx_product_rows_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __
       const int i = lane / MT, r = lane % MT;
       float v = 0.f;
       for (int k = 0; k < k_warps; ++k) v += part[warp + k][lane];
-      if (n0 + i < N && m0 + r < M) y[(m0 + r) * y_stride + n0 + i] = from_float<T>(v * (4.f * X::UNIT) + (bias ? bias[n0 + i] : 0.f));
+      if constexpr (FUSED) {
+        v = v * (4.f * X::UNIT) + (bias && n0 + i < N ? bias[weight_row<true>(tail, n0 + i, N)] : 0.f);
+        int o = n0 + i;
+        if (tail.gated) {                          // lanes below MT have the gates, MT lanes further on is what each multiplies
+          const float up = __shfl_down_sync((1u << R * MT) - 1u, v, MT);
+          mx_activate<1>(&v, tail.act);
+          v *= up;
+          o = i == 0 ? n0 >> 1 : N;
+        } else {
+          mx_activate<1>(&v, tail.act);
+        }
+        if (o < N >> tail.gated && m0 + r < M) {
+          if (tail.residual) v += to_float(static_cast<const T*>(tail.residual)[(m0 + r) * tail.r_stride + o]);
+          y[(m0 + r) * y_stride + o] = from_float<T>(v);
+        }
+      } else {
+        if (n0 + i < N && m0 + r < M) y[(m0 + r) * y_stride + n0 + i] = from_float<T>(v * (4.f * X::UNIT) + (bias ? bias[n0 + i] : 0.f));
+      }
     }
     if (k_warps > 1) __syncthreads(); else __syncwarp();
   }
 }
 
-template <int MT, int U, typename X, typename T>
+template <int MT, int U, bool FUSED, typename X, typename T>
 aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
   const int64_t row_bytes = mx_row_bytes(p.K), scale_row = mx_scale_row_bytes(p.K);
   // Warps along k until a warp's share is one round of loads, as long as that gives blocks to SMs without: one row, 4096 x 4096, 12.0 us
@@ -409,18 +437,19 @@ aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
     k_warps *= 2;
   const int per_block = kMxThreads / 32 / k_warps * kRowChannels;
   const dim3 grid((p.N + per_block - 1) / per_block, min((p.M + MT - 1) / MT, 65535));
-  mx_product_rows_kernel<X, T, MT, U><<<grid, kMxThreads, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N, p.K, p.M,
-                                                                 k_warps, static_cast<T*>(p.y), p.y_stride);
+  mx_product_rows_kernel<X, T, MT, U, FUSED><<<grid, kMxThreads, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N, p.K, p.M,
+                                                                        k_warps, static_cast<T*>(p.y), p.y_stride,
+                                                                        MxTail{p.act, p.gated, p.residual, p.r_stride});
   AIQ_LAUNCH_CHECK("mx_product_rows");
   return AIQ_OK;
 }
-template <typename X, typename T>
+template <bool FUSED, typename X, typename T>
 aiq_status_t product_rows(const MxProduct& p, X x, cudaStream_t s) {
   LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * p.M * p.N * p.K,
                     (double)(p.N + (p.x ? 0 : p.M)) * (mx_row_bytes(p.K) + mx_scale_row_bytes(p.K)) + sizeof(T) * (double)p.M * (p.N + (p.x ? p.K : 0)));
-  if (p.M == 1) return product_rows<1, 4, X, T>(p, x, s);
-  if (p.M == 2) return product_rows<2, 2, X, T>(p, x, s);
-  return product_rows<4, 2, X, T>(p, x, s);
+  if (p.M == 1) return product_rows<1, 4, FUSED, X, T>(p, x, s);
+  if (p.M == 2) return product_rows<2, 2, FUSED, X, T>(p, x, s);
+  return product_rows<4, 2, FUSED, X, T>(p, x, s);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -623,10 +652,10 @@ struct OneHeld {                                 // x microscaled
   }
 };
 
-template <typename X, typename T>
+template <typename X, typename T, bool FUSED>
 __global__ void __launch_bounds__(32 * kOneWarps, X::P == 1 ? 2 : 1)
 mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t row_bytes, int64_t scale_row,
-                      const float* __restrict__ bias, int N, int K, int channels, T* __restrict__ y) {
+                      const float* __restrict__ bias, int N, int K, int channels, T* __restrict__ y, MxTail tail) {
   constexpr int R = kOneRow, P = X::P;
   __shared__ float part[kOneChannels * kOneWarps];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, warps = blockDim.x >> 5;
@@ -641,7 +670,7 @@ mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __r
     auto load = [&](int n) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        const int64_t row = min(n0 + n + i, N - 1);
+        const int64_t row = weight_row<FUSED>(tail, min(n0 + n + i, N - 1), N);
         next[i] = __ldcs(reinterpret_cast<const uint4*>(codes + row * row_bytes + at16));
         next_s[i] = *(scales + row * scale_row + at);
       }
@@ -702,6 +731,23 @@ mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __r
     }
   }
   __syncthreads();
+  if constexpr (FUSED) {
+    // n0 and n_end are even with a gate: channels come in fours, and N is even
+    for (int n = threadIdx.x << tail.gated; n < n_end; n += blockDim.x << tail.gated) {
+      float v = bias ? bias[weight_row<true>(tail, n0 + n, N)] : 0.f;
+      for (int w = 0; w < warps; ++w) v += part[n * warps + w];
+      mx_activate<1>(&v, tail.act);
+      if (tail.gated) {
+        float up = bias ? bias[weight_row<true>(tail, n0 + n + 1, N)] : 0.f;
+        for (int w = 0; w < warps; ++w) up += part[(n + 1) * warps + w];
+        v *= up;
+      }
+      const int o = (n0 + n) >> tail.gated;
+      if (tail.residual) v += to_float(static_cast<const T*>(tail.residual)[o]);
+      y[o] = from_float<T>(v);
+    }
+    return;
+  }
   for (int n = threadIdx.x; n < n_end; n += blockDim.x) {
     float v = 0.f;
     for (int w = 0; w < warps; ++w) v += part[n * warps + w];
@@ -709,7 +755,7 @@ mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __r
   }
 }
 
-template <typename X, typename T>
+template <bool FUSED, typename X, typename T>
 aiq_status_t product_row(const MxProduct& p, X x, cudaStream_t s) {
   DeviceProps props;
   if (aiq_status_t st = current_device_props(&props)) return st;
@@ -719,22 +765,25 @@ aiq_status_t product_row(const MxProduct& p, X x, cudaStream_t s) {
   const int channels = min(kOneChannels, ((p.N + ctas - 1) / ctas + kOneRow - 1) / kOneRow * kOneRow);
   LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * p.N * p.K,
                     (double)(p.N + (p.x ? 0 : 1)) * (row_bytes + scale_row) + sizeof(T) * (double)(p.N + (p.x ? p.K : 0)));
-  mx_product_row_kernel<X, T><<<(p.N + channels - 1) / channels, 32 * warps, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N, p.K,
-                                                                                    channels, static_cast<T*>(p.y));
+  mx_product_row_kernel<X, T, FUSED><<<(p.N + channels - 1) / channels, 32 * warps, 0, s>>>(x, p.w_codes, p.w_scales, row_bytes, scale_row, p.bias, p.N,
+                                                                                           p.K, channels, static_cast<T*>(p.y),
+                                                                                           MxTail{p.act, p.gated, p.residual, p.r_stride});
   AIQ_LAUNCH_CHECK("mx_product_row");
   return AIQ_OK;
 }
 
-template <typename T>
+template <typename T, bool FUSED>
 aiq_status_t product_rows(const MxProduct& p, cudaStream_t s) {
-  if (p.x) {
+  if (FUSED || p.x) {
     const bool vec = (((uintptr_t)p.x) & 15) == 0 && (p.M == 1 || p.x_stride * (int64_t)sizeof(T) % 16 == 0);
     if constexpr (sizeof(T) == 2)
-      if (p.M == 1 && (int64_t)p.N * p.K > kOneFrom) return product_row<OneOf<T>, T>(p, OneOf<T>{static_cast<const T*>(p.x), vec}, s);
-    return product_rows<RowsOf<T>, T>(p, RowsOf<T>{static_cast<const T*>(p.x), p.x_stride, vec}, s);
+      if (p.M == 1 && (int64_t)p.N * p.K > kOneFrom) return product_row<FUSED, OneOf<T>, T>(p, OneOf<T>{static_cast<const T*>(p.x), vec}, s);
+    return product_rows<FUSED, RowsOf<T>, T>(p, RowsOf<T>{static_cast<const T*>(p.x), p.x_stride, vec}, s);
   }
-  if (p.M == 1) return product_row<OneHeld, T>(p, OneHeld{p.x_codes, p.x_scales}, s);
-  return product_rows<RowsHeld, T>(p, RowsHeld{p.x_codes, p.x_scales, mx_row_bytes(p.K), mx_scale_row_bytes(p.K)}, s);
+  if constexpr (!FUSED) {
+    if (p.M == 1) return product_row<false, OneHeld, T>(p, OneHeld{p.x_codes, p.x_scales}, s);
+    return product_rows<false, RowsHeld, T>(p, RowsHeld{p.x_codes, p.x_scales, mx_row_bytes(p.K), mx_scale_row_bytes(p.K)}, s);
+  }
 }
 
 }  // namespace
@@ -759,9 +808,16 @@ aiq_status_t launch_mx_dequantize(const uint8_t* codes, const uint8_t* scales, i
 
 aiq_status_t launch_mx_product_rows(const MxProduct& p, cudaStream_t s) {
   switch (p.dtype) {
-    case AIQ_DTYPE_F32: return product_rows<float>(p, s);
-    case AIQ_DTYPE_F16: return product_rows<__half>(p, s);
-    default: return product_rows<__nv_bfloat16>(p, s);
+    case AIQ_DTYPE_F32: return product_rows<float, false>(p, s);
+    case AIQ_DTYPE_F16: return product_rows<__half, false>(p, s);
+    default: return product_rows<__nv_bfloat16, false>(p, s);
+  }
+}
+aiq_status_t launch_mx_linear_act_rows(const MxProduct& p, cudaStream_t s) {
+  switch (p.dtype) {
+    case AIQ_DTYPE_F32: return product_rows<float, true>(p, s);
+    case AIQ_DTYPE_F16: return product_rows<__half, true>(p, s);
+    default: return product_rows<__nv_bfloat16, true>(p, s);
   }
 }
 
@@ -796,6 +852,13 @@ static aiq_status_t mx_check_rows(const char* what, const void* p, int dtype, in
 static aiq_status_t mx_check_out(const char* what, const void* p, int dtype, int rows, int K, int64_t stride) {
   if (aiq_status_t st = mx_check_rows(what, p, dtype, stride)) return st;
   if (rows > 1 && stride < K) return set_error(AIQ_ERR_INVALID_ARG, "%s: output row stride %lld < %d", what, (long long)stride, K);
+  return AIQ_OK;
+}
+
+static aiq_status_t mx_check_tail(const char* what, int activation, int gated, int N) {
+  if (activation < AIQ_ACT_NONE || activation > AIQ_ACT_GELU_TANH) return set_error(AIQ_ERR_INVALID_ARG, "%s: activation=%d", what, activation);
+  if (gated != 0 && gated != 1) return set_error(AIQ_ERR_INVALID_ARG, "%s: gated=%d", what, gated);
+  if (gated && (N & 1)) return set_error(AIQ_ERR_INVALID_ARG, "%s: gated with N=%d", what, N);
   return AIQ_OK;
 }
 
@@ -860,6 +923,37 @@ extern "C" aiq_status_t aiq_mx_linear(const void* codes, const void* scales, con
   if (aiq_status_t st = aiq::check_device_sm100()) return st;
   if (needed == 0 || !workspace) return aiq::launch_mx_product_rows(p, (cudaStream_t)stream);
   return aiq::launch_mx_product_tc(p, workspace, (cudaStream_t)stream);
+}
+
+extern "C" aiq_status_t aiq_mx_linear_act(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
+                                          int M, int64_t x_stride, int activation, int gated, const void* residual, int64_t r_stride, void* y,
+                                          int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  if (aiq_status_t st = mx_check("aiq_mx_linear_act", codes, scales, N, K)) return st;
+  if (M <= 0 || M > kMxMost) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear_act: M=%d", M);
+  if (aiq_status_t st = mx_check_tail("aiq_mx_linear_act", activation, gated, N)) return st;
+  const int outputs = gated ? N / 2 : N;
+  if (M == 1) { x_stride = K; y_stride = r_stride = outputs; }
+  if (aiq_status_t st = mx_check_rows("aiq_mx_linear_act", x, dtype, x_stride)) return st;
+  if (aiq_status_t st = mx_check_out("aiq_mx_linear_act", y, dtype, M, outputs, y_stride)) return st;
+  if (aiq_status_t st = mx_check_bias("aiq_mx_linear_act", bias)) return st;
+  if (residual)
+    if (aiq_status_t st = mx_check_rows("aiq_mx_linear_act", residual, dtype, r_stride)) return st;
+  aiq::MxProduct p = {};
+  p.w_codes = static_cast<const uint8_t*>(codes);
+  p.w_scales = static_cast<const uint8_t*>(scales);
+  p.bias = bias;
+  p.x = x; p.x_stride = x_stride;
+  p.y = y; p.y_stride = y_stride;
+  p.N = N; p.K = K; p.M = M; p.dtype = dtype;
+  p.act = activation; p.gated = gated;
+  p.residual = residual; p.r_stride = r_stride;
+  if (((uintptr_t)workspace) & 15) return set_error(AIQ_ERR_INVALID_ARG, "aiq_mx_linear_act: workspace not 16-byte aligned");
+  const size_t needed = aiq_mx_linear_workspace_bytes(N, K, M, dtype);
+  if (workspace && workspace_bytes < needed)
+    return set_error(AIQ_ERR_WORKSPACE_TOO_SMALL, "aiq_mx_linear_act: workspace of %zu bytes, %zu needed", workspace_bytes, needed);
+  if (aiq_status_t st = aiq::check_device_sm100()) return st;
+  if (needed == 0 || !workspace) return aiq::launch_mx_linear_act_rows(p, (cudaStream_t)stream);
+  return aiq::launch_mx_linear_act_tc(p, workspace, (cudaStream_t)stream);
 }
 
 extern "C" aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales, int M, const void* b_codes, const void* b_scales, int N,

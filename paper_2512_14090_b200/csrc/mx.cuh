@@ -16,6 +16,12 @@ inline size_t mx_dtype_bytes(int dtype) { return dtype == AIQ_DTYPE_F32 ? 4 : 2;
 inline int64_t mx_row_bytes(int K) { return ((int64_t)K + 127) / 128 * 64; }
 inline int64_t mx_scale_row_bytes(int K) { return ((int64_t)K + 511) / 512 * 16; }
 
+// A block of rows of one expert in an expert plan, aligned like an int4: blocks `first` to first + ceil(rows / width) - 1 are this expert's, whose
+// rows are `begin` to begin + rows - 1.
+struct __align__(16) ExpertBlock {
+  int expert, begin, rows, first;
+};
+
 // One product: y[m][n] = sum_k x[m][k] W[n][k] + bias[n]
 struct MxProduct {
   const uint8_t* w_codes;
@@ -27,6 +33,16 @@ struct MxProduct {
   void* y;                    // [M] rows of `y_stride` elements of `dtype`
   int64_t x_stride, y_stride;
   int N, K, M, dtype;
+  // aiq_mx_linear_act, aiq_mx_linear_experts: y = act(product), or with `gated` act(channels n) * (channels N / 2 + n), plus residual
+  int act, gated;
+  const void* residual;       // [M] rows of `r_stride` elements, or nullptr
+  int64_t r_stride;
+  // aiq_mx_linear_experts: weights [experts][N], M rows at most
+  int experts, top_k, width, blocks_most;
+  const int* header;          // of the plan: rows, blocks, and
+  int tokens, plan_kind;      //   what tells that it is one of these sizes
+  const ExpertBlock* blocks;
+  const int* positions;       // [M / top_k][top_k] rows of each token, or nullptr: x has the plan's rows
 };
 
 // ---- launchers ------------------------------------------------------------------------
@@ -39,7 +55,14 @@ aiq_status_t launch_mx_product_rows(const MxProduct& p, cudaStream_t s);
 // tensor cores (mx_tc.cu); with x not microscaled: needs the workspace, for x as eight-bit pieces
 size_t mx_tc_workspace_bytes(int K, int M, int dtype);
 aiq_status_t launch_mx_product_tc(const MxProduct& p, void* workspace, cudaStream_t s);
+aiq_status_t launch_mx_linear_act_rows(const MxProduct& p, cudaStream_t s);
+aiq_status_t launch_mx_linear_act_tc(const MxProduct& p, void* workspace, cudaStream_t s);        // mx_act.cu
+aiq_status_t launch_mx_linear_experts(const MxProduct& p, void* workspace, cudaStream_t s);       // mx_experts.cu
 void mx_tc_expire_next(int64_t limit_cycles);      // see aiq_debug_mx_expire_wait
+long long mx_tc_expire_cycles();
+struct MxExpireOnce {                               // held by a call that took the request up
+  ~MxExpireOnce() { mx_tc_expire_next(0); }
+};
 
 // ---- device helpers -------------------------------------------------------------------
 // 2^(s - 127) as a float; NaN for 255
@@ -86,6 +109,27 @@ template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// C values through an AIQ_ACT_*.  Comparisons, not fmaxf: a NaN stays one.  x times a logistic function of x (SILU) or of 2 sqrt(2/pi) (x + 0.044715 x^3),
+// since (1 + tanh u) / 2 = 1 / (1 + exp(-2u)); the error function's complement, so that nothing is cancelled left of zero.  All in float32.
+template <int C>
+__device__ __forceinline__ void mx_activate(float* v, int act) {
+  if (act == AIQ_ACT_NONE) return;
+  if (act == AIQ_ACT_RELU || act == AIQ_ACT_RELU6) {
+    const float top = act == AIQ_ACT_RELU6 ? 6.f : __int_as_float(0x7F800000);
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = v[j] < 0.f ? 0.f : v[j] > top ? top : v[j];
+  } else if (act == AIQ_ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = 0.5f * v[j] * erfcf(v[j] * -0.70710678118654752f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const float u = act == AIQ_ACT_SILU ? v[j] : v[j] * (1.5957691216057308f + 0.071354816272600248f * v[j] * v[j]);
+      v[j] = __fdividef(v[j], 1.f + expf(-u));
+    }
+  }
+}
 
 // eight consecutive values from a 16-byte aligned address (float: two loads)
 template <typename T>

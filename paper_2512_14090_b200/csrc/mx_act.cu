@@ -1,0 +1,16 @@
+// The linear layer with an activation, a gate and a residual on the tensor cores: see mx_tc.cuh, MODE 1.
+#include "mx_tc.cuh"
+
+namespace aiq {
+
+aiq_status_t launch_mx_linear_act_tc(const MxProduct& p, void* workspace, cudaStream_t s) {
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  MxExpireOnce once;
+  switch (p.dtype) {
+    case AIQ_DTYPE_F32: return launch_kind<1, float, 1>(p, ws, s);
+    case AIQ_DTYPE_F16: return launch_kind<1, __half, 1>(p, ws, s);
+    default: return launch_kind<1, __nv_bfloat16, 1>(p, ws, s);
+  }
+}
+
+}  // namespace aiq

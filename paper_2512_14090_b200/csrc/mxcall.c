@@ -71,11 +71,83 @@ static PyObject* matmul(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+static PyObject* linear_act(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  long long v[18];
+  int status;
+  (void)self;
+  if (!take("aiq_mx_linear_act", args, n, 18, v)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = aiq_mx_linear_act(PTR(0), PTR(1), (const float*)PTR(2), INT(3), INT(4), PTR(5), INT(6), INT(7), v[8], INT(9), INT(10), PTR(11), v[12],
+                             PTR(13), v[14], PTR(15), (size_t)v[16], PTR(17));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+static PyObject* plan_experts(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  long long v[7];
+  int status;
+  (void)self;
+  if (!take("aiq_plan_experts", args, n, 7, v)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = aiq_plan_experts((const int32_t*)PTR(0), INT(1), INT(2), INT(3), PTR(4), (size_t)v[5], PTR(6));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+/* the one with a float among its arguments */
+static PyObject* route_experts(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  enum { SCALE = 12, N = 18 };
+  PyObject* whole[N];
+  long long v[N];
+  double scale;
+  int status;
+  (void)self;
+  if (n != N) return take("aiq_route_experts", args, n, N, v), NULL;
+  for (Py_ssize_t i = 0; i < N; ++i) whole[i] = i == SCALE ? Py_None : args[i];
+  if (!take("aiq_route_experts", whole, N, N, v)) return NULL;
+  scale = PyFloat_AsDouble(args[SCALE]);
+  if (scale == -1.0 && PyErr_Occurred()) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = aiq_route_experts(PTR(0), INT(1), INT(2), INT(3), v[4], (const float*)PTR(5), INT(6), INT(7), INT(8), INT(9), INT(10), INT(11), (float)scale,
+                             (int32_t*)PTR(13), (float*)PTR(14), PTR(15), (size_t)v[16], PTR(17));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+static PyObject* linear_experts(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  long long v[21];
+  int status;
+  (void)self;
+  if (!take("aiq_mx_linear_experts", args, n, 21, v)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = aiq_mx_linear_experts(PTR(0), PTR(1), (const float*)PTR(2), INT(3), INT(4), INT(5), PTR(6), INT(7), v[8], INT(9), PTR(10), (size_t)v[11], INT(12),
+                                 INT(13), INT(14), INT(15), PTR(16), v[17], PTR(18), (size_t)v[19], PTR(20));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+static PyObject* combine_experts(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  long long v[15];
+  int status;
+  (void)self;
+  if (!take("aiq_combine_experts", args, n, 15, v)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = aiq_combine_experts(PTR(0), INT(1), INT(2), INT(3), INT(4), INT(5), v[6], (const float*)PTR(7), PTR(8), (size_t)v[9], PTR(10), v[11], PTR(12),
+                               v[13], PTR(14));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
 static PyMethodDef methods[] = {
     {"aiq_mx_quantize", (PyCFunction)(void (*)(void))quantize, METH_FASTCALL, NULL},
     {"aiq_mx_dequantize", (PyCFunction)(void (*)(void))dequantize, METH_FASTCALL, NULL},
     {"aiq_mx_linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, NULL},
     {"aiq_mx_matmul", (PyCFunction)(void (*)(void))matmul, METH_FASTCALL, NULL},
+    {"aiq_mx_linear_act", (PyCFunction)(void (*)(void))linear_act, METH_FASTCALL, NULL},
+    {"aiq_plan_experts", (PyCFunction)(void (*)(void))plan_experts, METH_FASTCALL, NULL},
+    {"aiq_route_experts", (PyCFunction)(void (*)(void))route_experts, METH_FASTCALL, NULL},
+    {"aiq_mx_linear_experts", (PyCFunction)(void (*)(void))linear_experts, METH_FASTCALL, NULL},
+    {"aiq_combine_experts", (PyCFunction)(void (*)(void))combine_experts, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mxcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__mxcall(void) { return PyModule_Create(&module); }
