@@ -598,7 +598,8 @@ def aiq_expert_plan_parts(plan, T, top_k, E):
         at = _mx_plans[key] = [a.value // 4 for a in starts]
     import torch
     w = plan.view(torch.int32)
-    return w[at[0]:at[0] + E + 1], w[at[1]:at[1] + T * top_k], w[at[2]:at[2] + T * top_k].view(T, top_k)
+    return (w.as_strided((E + 1,), (1,), w.storage_offset() + at[0]), w.as_strided((T * top_k,), (1,), w.storage_offset() + at[1]),
+            w.as_strided((T, top_k), (top_k, 1), w.storage_offset() + at[2]))
 
 
 def aiq_plan_experts(ids, E, plan, stream=None):
