@@ -69,7 +69,10 @@ struct MxTcParams {
   int pieces;               // KIND 1: eight-bit pieces of x
   int stack;                // 1: the pieces' rows are one operand
   int rows;                 // rows of a B operand: Mt, stacked pieces * Mt
+  int join;                 // MODE 2: a copy brings all pieces of a chunk (up to three fit)
+  int ring_rows;            // rows that a slot of the ring for x holds: `rows`, joined those of all pieces
   int n_chunks, supers_per_split;
+  int group;                // MODE 1, 2: chunks per copy and slot of the rings
   int cluster, cluster_log2;
   int push;                 // bytes for sums that the cluster's CTAs write into each other's shared memory; 0: read from it afterwards
   int m_blocks, tiles;      // tiles: row blocks * m_blocks, then the halves of some of them:
@@ -117,7 +120,7 @@ __device__ __forceinline__ MxTile mx_expert_tile(const MxTcParams& p, const Expe
 __host__ __device__ inline int mx_b_unit(int rows) { return rows * 128; }
 // rings of codes; with a split K range the sums of the tile, [row of x][128 channels], in their place afterwards or behind them
 __host__ __device__ inline int mx_ring_bytes(const MxTcParams& p) {
-  const int rings = p.a_stages * kMxATile + p.b_stages * mx_b_unit(p.rows), sums = p.cluster > 1 && !p.push ? p.Mt * 128 * 4 : 0;
+  const int rings = p.group * (p.a_stages * kMxATile + p.b_stages * mx_b_unit(p.ring_rows)), sums = p.cluster > 1 && !p.push ? p.Mt * 128 * 4 : 0;
   return (rings > sums ? rings : sums) + p.push;
 }
 __host__ __device__ inline int mx_scale_tile(const MxTcParams& p) { return (128 + p.b_cols * 32 * (p.stack ? 1 : p.pieces)) * 16; }
@@ -158,6 +161,19 @@ __device__ __forceinline__ void mx_mma4(uint32_t d, uint64_t a, uint64_t b, uint
         "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n\t"
         "@r tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%8];\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate), "r"(bar_b), "r"(bar_a) : "memory");
+}
+// KIND 1, without commits
+__device__ __forceinline__ void mx_mma4_more(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 x, y;\n\t.reg .b32 i;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+      "add.s64 x, %1, 2;\n\tadd.s64 y, %2, 2;\n\tadd.u32 i, %3, 0x20000010;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], x, y, i, [%4], [%5], 1;\n\t"
+      "add.s64 x, %1, 4;\n\tadd.s64 y, %2, 4;\n\tadd.u32 i, %3, 0x40000020;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], x, y, i, [%4], [%5], 1;\n\t"
+      "add.s64 x, %1, 6;\n\tadd.s64 y, %2, 6;\n\tadd.u32 i, %3, 0x60000030;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], x, y, i, [%4], [%5], 1;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -238,7 +254,14 @@ __device__ __forceinline__ void store_columns(T* dst, int64_t y_stride, const fl
   }
 }
 
-// ---- MODE 1, 2: the way out ----
+// ---- MODE 1, 2: copies of several chunks, MMAs whose commits may be left out, the way out ----
+__device__ __forceinline__ void tma_fill_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar, uint32_t bytes, int c0, int c1, int c2, int c3, int c4) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+      "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%2], %3;\n\t"
+      "@q cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%4, %5, %6, %7, %8}], [%2];\n\t}"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(bytes), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
+}
 __device__ __forceinline__ void tma_fill_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, uint32_t bytes, int c0, int c1, int c2, int c3) {
   asm volatile(
       "{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
@@ -246,12 +269,21 @@ __device__ __forceinline__ void tma_fill_4d(uint32_t dst, const CUtensorMap* map
       "@q cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%4, %5, %6, %7}], [%2];\n\t}"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(bytes), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
-// C columns of a lane's channel, sums with their bias, to what y gets.  row: of the first column in y, end: the first one behind those that are
-// written (0: none); o: the lane's output; all lanes of the warp take part.  With a gate, lanes 2i and 2i + 1 hold gate and factor of output i: one
-// exchange gives the even lane both for an even column, the odd lane for the odd one beside it.
+// The residual of C columns of a lane's channel, from row `row` on; with a gate of every other column from `row` + (lane & 1) on.
 template <int C, typename T>
-__device__ __forceinline__ void finish_columns(float* f, int act, int gated, int lane, int row, int end, T* y, int64_t y_stride, const T* residual,
-                                               int64_t r_stride, int o) {
+__device__ __forceinline__ void load_residual(T* r, int gated, int lane, int row, int end, const T* residual, int64_t r_stride, int o) {
+  const int first = gated ? row + (lane & 1) : row, step = 1 << gated, live = end - first;
+  const T* src = residual + (int64_t)first * r_stride + o;
+  const int64_t stride = r_stride << gated;
+#pragma unroll
+  for (int j = 0; j < C; ++j)
+    if (j * step < live && (j < C / 2 || !gated)) r[j] = src[j * stride];
+}
+// C columns of a lane's channel, sums with their bias, to what y gets.  row: of the first column in y, end: the first one behind those that are
+// written (0: none); o: the lane's output; r: what load_residual has brought, or nullptr; all lanes of the warp take part.  With a gate, lanes 2i and
+// 2i + 1 hold gate and factor of output i: one exchange gives the even lane both for an even column, the odd lane for the odd one beside it.
+template <int C, typename T>
+__device__ __forceinline__ void finish_columns(float* f, int act, int gated, int lane, int row, int end, T* y, int64_t y_stride, const T* r, bool has_residual, int o) {
   if (gated) {
     const int odd = lane & 1;
     float up[C / 2];
@@ -264,18 +296,12 @@ __device__ __forceinline__ void finish_columns(float* f, int act, int gated, int
     mx_activate<C / 2>(f, act);
 #pragma unroll
     for (int j = 0; j < C / 2; ++j) f[j] *= up[j];
+    if (has_residual) {
+#pragma unroll
+      for (int j = 0; j < C / 2; ++j) f[j] += to_float(r[j]);
+    }
     const int64_t first = row + odd;
     const int live = end - (int)first;
-    if (residual) {
-      T r[C / 2];
-      const T* src = residual + first * r_stride + o;
-#pragma unroll
-      for (int j = 0; j < C / 2; ++j)
-        if (2 * j < live) r[j] = src[2 * j * r_stride];
-#pragma unroll
-      for (int j = 0; j < C / 2; ++j)
-        if (2 * j < live) f[j] += to_float(r[j]);
-    }
     T* dst = y + first * y_stride + o;
 #pragma unroll
     for (int j = 0; j < C / 2; ++j) {
@@ -284,18 +310,12 @@ __device__ __forceinline__ void finish_columns(float* f, int act, int gated, int
     }
   } else {
     mx_activate<C>(f, act);
-    const int live = end - row;
-    if (residual) {
-      T r[C];
-      const T* src = residual + row * r_stride + o;
+    if (has_residual) {
 #pragma unroll
-      for (int j = 0; j < C; ++j)
-        if (j < live) r[j] = src[j * r_stride];
-#pragma unroll
-      for (int j = 0; j < C; ++j)
-        if (j < live) f[j] += to_float(r[j]);
+      for (int j = 0; j < C; ++j) f[j] += to_float(r[j]);
     }
-    T* dst = y + row * y_stride + o;
+    const int live = end - row;
+    T* dst = y + (int64_t)row * y_stride + o;
 #pragma unroll
     for (int j = 0; j < C; ++j) {
       if (j < live) *dst = from_float<T>(f[j]);
@@ -372,8 +392,10 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int rank = blockIdx.x & (p.cluster - 1);
   const int first = blockIdx.x >> p.cluster_log2, step = gridDim.x >> p.cluster_log2;      // this CTA's tiles
-  const int a_stages = p.a_stages, b_stages = p.b_stages, units = p.stack ? 1 : p.pieces;
-  const int b_unit = mx_b_unit(p.rows), scale_tile = mx_scale_tile(p);
+  const int a_stages = p.a_stages, b_stages = p.b_stages, scale_units = p.stack ? 1 : p.pieces;
+  const int units = MODE == 2 && p.join ? 1 : scale_units;   // copies of a chunk of x
+  const int group = MODE == 0 ? 1 : p.group, a_unit = group * kMxATile;
+  const int b_unit = group * mx_b_unit(p.ring_rows), scale_tile = mx_scale_tile(p);
   const int c_begin = min(p.n_chunks, rank * p.supers_per_split * Kd::CPS);
   const int c_end = min(p.n_chunks, c_begin + p.supers_per_split * Kd::CPS);
   const int chunks = c_end - c_begin, supers = (chunks + Kd::CPS - 1) / Kd::CPS;
@@ -389,11 +411,11 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     else return mx_tile(p, t);
   };
   // copies of rows of x for a tile, and the rows they bring
-  auto boxes_of = [&](const MxTile& at) { return MODE == 2 ? (p.stack ? 1 : (at.Mt + p.box - 1) / p.box) : at.Mt > p.box ? 2 : 1; };
-  auto rows_of = [&](const MxTile& at) { return MODE == 2 ? boxes_of(at) * p.box : at.Mt; };
+  auto boxes_of = [&](const MxTile& at) { return MODE != 2 && at.Mt > p.box ? 2 : 1; };
+  auto rows_of = [&](const MxTile& at) { return MODE == 2 ? p.box : at.Mt; };
 
   uint8_t* aring = smem;
-  uint8_t* bring = aring + a_stages * kMxATile;
+  uint8_t* bring = aring + a_stages * a_unit;
   uint8_t* sring = smem + mx_ring_bytes(p);
   uint64_t* bars = reinterpret_cast<uint64_t*>(sring + kMxScaleStages * scale_tile);
   const uint32_t a_full = smem_u32(bars), a_empty = a_full + 8 * a_stages;
@@ -417,11 +439,12 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   auto send_a = [&]() {
     if constexpr (MODE == 0)
       tma_fill_2d(smem_u32(aring) + ar.stage * kMxATile, &a_map, a_full + 8 * ar.stage, KIND == 0 ? kMxATile : kMxACopied, a_chunk * 128, a_n0);
+    else if (group == 1)
+      tma_fill_4d(smem_u32(aring) + ar.stage * a_unit, &a_map, a_full + 8 * ar.stage, kMxACopied, a_chunk * 128, 0, a_n0 >> p.gated, a_expert);
     else
-      tma_fill_4d(smem_u32(aring) + ar.stage * kMxATile, &a_map, a_full + 8 * ar.stage, KIND == 0 ? kMxATile : kMxACopied, a_chunk * 128, 0,
-                  a_n0 >> p.gated, a_expert);
+      tma_fill_5d(smem_u32(aring) + ar.stage * a_unit, &a_map, a_full + 8 * ar.stage, group * kMxACopied, 0, 0, a_n0 >> p.gated, a_expert, a_chunk);
     ar.sent(a_stages);
-    if (++a_chunk == c_end) {
+    if ((a_chunk += group) >= c_end) {
       a_chunk = c_begin;
       a_tile += step;
       if (MODE == 0) {
@@ -441,7 +464,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
     if (chunks > 0 && first < tiles) {
-      const uint32_t bytes = (uint32_t)((128 + (p.stack ? p.rows : rows_of(tile_of(first)) * units)) * 16);
+      const uint32_t bytes = (uint32_t)((128 + (p.stack ? p.rows : rows_of(tile_of(first)) * scale_units)) * 16);
       if constexpr (MODE == 0) tma_fill_2d(smem_u32(sring), &sa_map, s_full, bytes, c_begin / Kd::CPS * 16, a_n0);
       else tma_fill_4d(smem_u32(sring), &sa_map, s_full, bytes, c_begin / Kd::CPS * 16, 0, a_n0 >> p.gated, a_expert);
     }
@@ -471,19 +494,16 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     RingCursor r;
     for (int tile = first; tile < tiles && alive; tile += step) {
       const MxTile at = tile_of(tile);
-      const int boxes = boxes_of(at), bytes = p.stack ? b_unit : rows_of(at) * 128;
+      const int boxes = boxes_of(at), bytes = MODE == 2 || p.stack ? mx_b_unit(p.ring_rows) : rows_of(at) * 128;
       for (int c0 = c_begin; c0 < c_end && alive; c0 += Kd::CPS)
         for (int u = units - 1; u >= 0 && alive; --u)
-          for (int c = c0; c < min(c0 + Kd::CPS, c_end); ++c) {
+          for (int c = c0; c < min(c0 + Kd::CPS, c_end); c += group) {
             alive = mx_wait(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort);
             if (!alive) break;
             const uint32_t dst = smem_u32(bring) + r.stage * b_unit;
-            tma_fill_3d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)bytes, c * 128, at.m0, u);
-            if constexpr (MODE == 2) {
-              for (int b = 1; b < boxes; ++b) tma_load_3d_elect(dst + b * p.box * 128, &b_map, b_full + 8 * r.stage, c * 128, at.m0 + b * p.box, u);
-            } else {
-              if (boxes == 2) tma_load_3d_elect(dst + p.box * 128, &b_map, b_full + 8 * r.stage, c * 128, at.m0 + p.box, u);
-            }
+            if (MODE == 0 || group == 1) tma_fill_3d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)bytes, c * 128, at.m0, u);
+            else tma_fill_4d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)(group * bytes), 0, at.m0, u, c);
+            if (MODE != 2 && boxes == 2) tma_load_3d_elect(dst + p.box * 128, &b_map, b_full + 8 * r.stage, c * 128, at.m0 + p.box, u);
             r.sent(b_stages);
           }
     }
@@ -493,7 +513,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     RingCursor r;
     for (int tile = first; tile < tiles && alive; tile += step) {
       const MxTile at = tile_of(tile);
-      const int boxes = boxes_of(at), bytes = (128 + (p.stack ? p.rows : rows_of(at) * units)) * 16;
+      const int boxes = boxes_of(at), bytes = (128 + (p.stack ? p.rows : rows_of(at) * scale_units)) * 16;
       for (int s = 0; s < supers; ++s) {
         alive = mx_wait(s_empty + 8 * r.stage, r.phase ^ 1u, s_abort);
         if (!alive) break;
@@ -507,7 +527,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
             tma_fill_4d(dst, &sa_map, bar, (uint32_t)bytes, byte, 0, at.n0 >> p.gated, at.expert);
           }
         }
-        for (int u = 0; u < units; ++u)
+        for (int u = 0; u < scale_units; ++u)
           for (int b = 0; b < boxes; ++b)
             tma_load_3d_elect(dst + (128 + u * p.b_cols * 32 + b * p.box) * 16, &sb_map, bar, byte, at.m0 + b * p.box, u);
         r.sent(kMxScaleStages);
@@ -543,24 +563,41 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
         const int n = min(Kd::CPS, chunks - s * Kd::CPS);
         for (int u = units - 1; u >= 0 && alive; --u) {
           uint32_t at = as, atph = aph;
-          for (int cc = 0; cc < n; ++cc) {
+          for (int cc = 0; cc < n; cc += group) {
             if (!ready) {
               alive = mbar_wait_uniform(a_full + 8 * at, atph, s_abort) && mbar_wait_uniform(b_full + 8 * bs, bph, s_abort);
               if (!alive) break;
             }
             tc_fence_after();
-            const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(aring) + at * kMxATile) >> 4) | LBO_FIELD);
+            const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(aring) + at * a_unit) >> 4) | LBO_FIELD);
             const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(((smem_u32(bring) + bs * b_unit) >> 4) | LBO_FIELD);
             const uint32_t sfa = sf + (KIND == 0 ? 2 * cc : cc) * p.sf_group, sfb = sfa + 4 + u * p.b_cols;
             const uint32_t b_done = b_empty + 8 * bs, a_done = u == 0 ? a_empty + 8 * at : 0u;
             if (++bs == (uint32_t)b_stages) { bs = 0; bph ^= 1u; }
             if (++at == (uint32_t)a_stages) { at = 0; atph ^= 1u; }
-            const bool last = cc + 1 == n;
+            const bool last = cc + group >= n;
             if (last && u == 0) { as = at; aph = atph; }
             const uint32_t na = last ? as : at, naph = last ? aph : atph;
             const bool next_ready = mbar_test(a_full + 8 * na, naph) & mbar_test(b_full + 8 * bs, bph);
             const bool next_t = last && u == 0 ? mbar_test(t_full + 8 * (tb ^ 1u), ((sets + 1) >> 1) & 1) : false;
-            mx_mma4<KIND>(d, adesc, bdesc, idesc, sfa, sfb, p.sf_group, accumulate, b_done, a_done);
+            if (MODE == 0 || (MODE == 1 && group == 1)) {
+              mx_mma4<KIND>(d, adesc, bdesc, idesc, sfa, sfb, p.sf_group, accumulate, b_done, a_done);
+            } else {
+              // all of the slot, a joined chunk's pieces one after the other, the smallest first; the last MMAs free the operands
+              const int q0 = MODE == 2 && p.join ? scale_units - 1 : 0, here = min(group, n - cc);
+              uint64_t ad = adesc, bd = bdesc;
+              uint32_t sa = sfa, sb = sfb;
+              for (int g = 0; g + 1 < here; ++g, ad += kMxATile >> 4, bd += p.ring_rows * 8, sa += p.sf_group, sb += p.sf_group)
+                for (int q = q0; q >= 0; --q) {
+                  mx_mma4_more(d, ad, bd + (uint64_t)(q * p.Mt * 8), idesc, sa, sb + q * p.b_cols, accumulate);
+                  accumulate = 1;
+                }
+              for (int q = q0; q > 0; --q) {
+                mx_mma4_more(d, ad, bd + (uint64_t)(q * p.Mt * 8), idesc, sa, sb + q * p.b_cols, accumulate);
+                accumulate = 1;
+              }
+              mx_mma4<KIND>(d, ad, bd, idesc, sa, sb, p.sf_group, accumulate, b_done, a_done);
+            }
             accumulate = 1;
             ready = __all_sync(0xffffffffu, next_ready);
             t_ready = __all_sync(0xffffffffu, next_t);
@@ -579,7 +616,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   } else if (warp < 8) {
     // ---- scale bytes -> tensor memory ----------------------------------------------------------------
     const uint32_t quarter = (uint32_t)(warp & 3) * 32;
-    const int cols = p.b_cols * units;
+    const int cols = p.b_cols * scale_units;
     const int sets = first < tiles ? ((tiles - 1 - first) / step + 1) * supers : 0;
     uint32_t stage = 0, phase = 0;
     for (int s = 0; s < sets; ++s) {
@@ -667,7 +704,9 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
                 if (c >= half) break;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[c + j] += b;
-                finish_columns<8, T>(acc + c, p.act, p.gated, lane, m0 + c, min(end, m0 + half), y, y_stride, ex.residual, ex.r_stride, o);
+                T r[8] = {};
+                if (ex.residual) load_residual<8, T>(r, p.gated, lane, m0 + c, min(end, m0 + half), ex.residual, ex.r_stride, o);
+                finish_columns<8, T>(acc + c, p.act, p.gated, lane, m0 + c, min(end, m0 + half), y, y_stride, r, ex.residual != nullptr, o);
               }
             }
           }
@@ -689,13 +728,48 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       } else {
         // Not unrolled: code that a block runs once per tile comes from far away (unrolled, 16 columns took 1,000 cycles).
         const uint32_t db = p.d_bufs == 2 ? done & 1 : 0, dph = (p.d_bufs == 2 ? done >> 1 : done) & 1;
+        // the residual of the next columns is asked for ahead: without that it took 88 us of 300 (8192 x 8192, 2,048 rows)
+        T ahead[MODE > 0 ? 8 : 1] = {};
+        if constexpr (MODE > 0)
+          if (direct && ex.residual) load_residual<8, T>(ahead, p.gated, lane, m0, end, ex.residual, ex.r_stride, o);
         if (supers > 0) alive = mx_wait(d_full + 8 * db, dph, s_abort);
         if (!alive) break;
         tc_fence_after();
+        bool released = false;
+        if constexpr (MODE > 0) {
+          // eight columns at a time: with 16 the kernel's registers were spilt, those of the warp that issues the MMAs among them
+          if (direct) {
+#pragma unroll 1
+            for (int c0 = 0; c0 < half; c0 += 8) {
+              float f[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f[j] = b;
+#pragma unroll 1
+              for (int q = copies - 1; q >= 0; --q) {
+                uint32_t v[8];
+                tmem_ld8(taddr + db * p.rows + q * p.Mt + c0, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(v[j]);
+              }
+              if (c0 + 8 == half) {                // the last of them is read: the next tile may have the columns
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(d_empty + 8 * db);
+                released = true;
+              }
+              T r[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) r[j] = ahead[j];
+              if (ex.residual && c0 + 8 < half) load_residual<8, T>(ahead, p.gated, lane, m0 + c0 + 8, end, ex.residual, ex.r_stride, o);
+              finish_columns<8, T>(f, p.act, p.gated, lane, m0 + c0, end, y, y_stride, r, ex.residual != nullptr, o);
+            }
+          }
+        }
         T* out = dst;
         int left = end - m0;
 #pragma unroll 1
-        for (int c0 = 0; c0 < half; c0 += 16) {
+        for (int c0 = 0; c0 < (MODE > 0 && direct ? 0 : half); c0 += 16) {
           float f[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) f[j] = b;
@@ -715,17 +789,17 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
           } else if (!direct) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) sums[(c0 + j) * 128] = f[j];
-          } else if constexpr (MODE > 0) {
-            finish_columns<16, T>(f, p.act, p.gated, lane, m0 + c0, end, y, y_stride, ex.residual, ex.r_stride, o);
-          } else {
+          } else if (MODE == 0) {
             store_columns<T>(out, y_stride, f, left);
             out += 16 * y_stride;
             left -= 16;
           }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(d_empty + 8 * db);
+        if (!released) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(d_empty + 8 * db);
+        }
       }
     }
   }
@@ -967,7 +1041,7 @@ aiq_status_t split_pairs(const MxProduct& p, uint8_t* planes, uint8_t* scales, c
 
 aiq_status_t encode(EncodeTiledFn enc, CUtensorMap* map, CUtensorMapDataType type, const void* base, int rank, const cuuint64_t* dims,
                     const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
-  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
   const CUresult r = enc(map, type, rank, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                          CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? AIQ_OK : set_error(AIQ_ERR_CUDA, "cuTensorMapEncodeTiled (microscaled product) failed with code %d", (int)r);
@@ -996,7 +1070,9 @@ aiq_status_t shape_experts(MxTcParams& p, const MxProduct& g, const MxShape& m) 
   p.Mt = g.width;
   p.stack = p.Mt <= 32;
   p.rows = p.stack ? p.Mt * p.pieces : p.Mt;
-  p.box = p.stack ? p.Mt : 32;
+  p.box = p.Mt;
+  p.join = p.stack || p.pieces <= 3;
+  p.ring_rows = p.join ? p.Mt * p.pieces : p.Mt;
   p.b_cols = ((p.rows + 31) / 32 + 3) / 4 * 4;
   p.sf_group = 4 + p.b_cols * (p.stack ? 1 : p.pieces);
   p.m_blocks = 1;
@@ -1087,8 +1163,11 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   while ((1 << p.cluster_log2) < p.cluster) ++p.cluster_log2;
   p.push = p.cluster > 1 && p.Mt <= 64 ? p.Mt * 512 : 0;       // Mt is a multiple of 16, the cluster has 2, 4 or 8 CTAs
   p.supers_per_split = (n_super + p.cluster - 1) / p.cluster;
-  const int chunks = p.supers_per_split * Kd::CPS, units = p.stack ? 1 : p.pieces;
-  p.a_stages = units > 1 ? Kd::CPS : 2;                        // the pieces of one set of chunks read the same weights
+  if (MODE != 2) p.ring_rows = p.rows;
+  p.group = 1;
+  if (MODE != 0 && (p.stack || p.join) && p.ring_rows <= 128 && p.supers_per_split * Kd::CPS > 1) p.group = 2;
+  const int chunks = (p.supers_per_split * Kd::CPS + p.group - 1) / p.group, units = p.stack || p.join ? 1 : p.pieces;
+  p.a_stages = units > 1 ? Kd::CPS / p.group : 2;              // the pieces of one set of chunks read the same weights
   p.b_stages = 2;
   auto fits = [&](int a, int b) { MxTcParams t = p; t.a_stages = a; t.b_stages = b; return mx_smem_bytes(t) <= props.smem_optin; };
   if (!fits(p.a_stages, p.b_stages)) return set_error(AIQ_ERR_SHAPE, "mx_tc: %d bytes of shared memory", mx_smem_bytes(p));
@@ -1104,10 +1183,11 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   CUtensorMap a_map, b_map, sa_map, sb_map;
   if constexpr (MODE != 0) {
     const cuuint64_t G = g.gated ? 2 : 1, E = MODE == 2 ? g.experts : 1;
-    const cuuint32_t box[4] = {128, (cuuint32_t)G, (cuuint32_t)(128 / G), 1}, sbox[4] = {16, (cuuint32_t)G, (cuuint32_t)(128 / G), 1};
-    const cuuint64_t dims[4] = {KIND == 0 ? w_row : 2 * w_row, G, N / G, E}, strides[3] = {N / G * w_row, w_row, N * w_row};
+    const cuuint32_t box[5] = {128, (cuuint32_t)G, (cuuint32_t)(128 / G), 1, (cuuint32_t)p.group}, sbox[4] = {16, (cuuint32_t)G, (cuuint32_t)(128 / G), 1};
+    // several chunks: the outermost dimension, so that they lie one behind the other in a slot
+    const cuuint64_t dims[5] = {p.group > 1 ? 128 : 2 * w_row, G, N / G, E, (cuuint64_t)p.n_chunks}, strides[4] = {N / G * w_row, w_row, N * w_row, 64};
     const cuuint64_t sdims[4] = {s_row, G, N / G, E}, sstrides[3] = {N / G * s_row, s_row, N * s_row};
-    if (aiq_status_t st = encode(enc, &a_map, KIND == 0 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, g.w_codes, 4,
+    if (aiq_status_t st = encode(enc, &a_map, KIND == 0 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, g.w_codes, p.group > 1 ? 5 : 4,
                                  dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
     if (aiq_status_t st = encode(enc, &sa_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.w_scales, 4, sdims, sstrides, sbox, CU_TENSOR_MAP_SWIZZLE_NONE))
       return st;
@@ -1126,9 +1206,10 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
     const uint8_t* codes = KIND == 0 ? g.x_codes : workspace;
 
     const uint8_t* scales = KIND == 0 ? g.x_scales : workspace + P * M * x_row;
-    const cuuint64_t dims[3] = {x_row, M, P}, strides[2] = {x_row, x_row * M};
-    const cuuint32_t box[3] = {128, (cuuint32_t)p.box, (cuuint32_t)(p.stack ? P : 1)};
-    if (aiq_status_t st = encode(enc, &b_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
+    const bool chunked = p.group > 1;
+    const cuuint64_t dims[4] = {chunked ? 128 : x_row, M, P, x_row / 128}, strides[3] = {x_row, x_row * M, 128};
+    const cuuint32_t box[4] = {128, (cuuint32_t)p.box, (cuuint32_t)(p.stack || p.join ? P : 1), (cuuint32_t)p.group};
+    if (aiq_status_t st = encode(enc, &b_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, chunked ? 4 : 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
     const cuuint64_t sdims[3] = {s_row, M, P}, sstrides[2] = {s_row, s_row * M};
     const cuuint32_t sbox[3] = {16, (cuuint32_t)p.box, (cuuint32_t)(p.stack ? P : 1)};
     if (aiq_status_t st = encode(enc, &sb_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, scales, 3, sdims, sstrides, sbox, CU_TENSOR_MAP_SWIZZLE_NONE))
