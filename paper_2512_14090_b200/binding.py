@@ -488,15 +488,6 @@ def _check_combine(z, weights, plan, e, y, residual):
     return dtype, t, top_k, width, z_stride, _expert_plan(plan, t, top_k, e), r_stride, y_stride
 
 
-def _bytes(t):
-    """What a check of a tensor without strides looks at."""
-    return (t.shape, t.dtype, t.is_contiguous()) if t is not None else None
-
-
-def _matrix(t):
-    return (t.shape, t.stride(), t.dtype) if t is not None else None
-
-
 def aiq_mx_row_bytes(K):
     return int(lib.aiq_mx_row_bytes(int(K)))
 
@@ -568,7 +559,9 @@ def aiq_mx_linear_act(codes, scales, bias, x, y, activation="none", gated=False,
     """y [M][N] = act(x W^T + bias) + residual; gated: y [M][N / 2] = act(x G^T + bias_g) * (x U^T + bias_u) + residual, G and U the first and the second
     half of the rows of W.  activation: "none", "relu", "relu6", "silu", "gelu" or "gelu_tanh"; residual as y, which it may be.  The rest as
     aiq_mx_linear, the workspace's size too."""
-    key = ("act", activation, gated, _bytes(codes), _bytes(scales), _bytes(bias), _matrix(x), _matrix(y), _matrix(residual))
+    key = (activation, gated, codes.shape, scales.shape, x.shape, y.shape, x.stride(), y.stride(), x.dtype, y.dtype, codes.dtype, scales.dtype,
+           codes.is_contiguous(), scales.is_contiguous(), (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None,
+           (residual.shape, residual.stride(), residual.dtype) if residual is not None else None)
     n, k, dtype, m, x_stride, act, gate, r_stride, y_stride = (
         _mx_plans.get(key) or _mx_plan(key, _mx_check_linear_act, codes, scales, bias, x, y, activation, gated, residual))
     d = x.get_device()
@@ -604,7 +597,7 @@ def aiq_expert_plan_parts(plan, T, top_k, E):
 
 def aiq_plan_experts(ids, E, plan, stream=None):
     """ids int32 [T][top_k] -> plan, a tensor of aiq_expert_plan_bytes(T, top_k, E) bytes."""
-    key = ("plan", E, _bytes(ids), _bytes(plan))
+    key = (E, ids.shape, ids.dtype, ids.is_contiguous(), plan.shape, plan.dtype, plan.is_contiguous())
     t, top_k, size = _mx_plans.get(key) or _mx_plan(key, _check_plan, ids, plan, int(E))
     d = ids.get_device()
     s = _mx_stream(stream, d, d == plan.get_device())
@@ -617,7 +610,9 @@ def aiq_route_experts(logits, ids, weights, bias=None, scoring="softmax", groups
                       stream=None):
     """logits [T][E] float32, float16 or bfloat16 -> ids int32 [T][top_k], weights float32 [T][top_k] and, where given, a plan of
     aiq_expert_plan_bytes(T, top_k, E) bytes.  scoring: "softmax" or "sigmoid"; bias float32 [E] or None."""
-    key = ("route", scoring, _matrix(logits), _bytes(ids), _bytes(weights), _bytes(bias), _bytes(plan))
+    key = (scoring, logits.shape, logits.stride(), logits.dtype, ids.shape, ids.dtype, ids.is_contiguous(), weights.shape, weights.dtype,
+           weights.is_contiguous(), (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None,
+           (plan.shape, plan.dtype, plan.is_contiguous()) if plan is not None else None)
     dtype, t, e, stride, score, top_k, size = _mx_plans.get(key) or _mx_plan(key, _check_route, logits, ids, weights, bias, scoring, plan)
     d = logits.get_device()
     s = _mx_stream(stream, d, d == ids.get_device() == weights.get_device() and (bias is None or bias.get_device() == d)
@@ -637,7 +632,9 @@ def aiq_mx_linear_experts(codes, scales, bias, x, plan, top_k, y, activation="no
     """y [T * top_k][N, gated: N / 2] = act(x W^T + bias) for the plan's rows, with each row's expert's weights: codes [E][N][aiq_mx_row_bytes(K)], scales
     [E][N][aiq_mx_scale_row_bytes(K)], bias float32 [E][N] or None.  x [T][K], or [T * top_k][K] in the plan's rows (x_sorted).  workspace: a tensor of
     aiq_mx_linear_experts_workspace_bytes(E, N, K, T * top_k, x.dtype) bytes."""
-    key = ("experts", activation, gated, x_sorted, top_k, _bytes(codes), _bytes(scales), _bytes(bias), _matrix(x), _matrix(y), _bytes(plan))
+    key = (activation, gated, x_sorted, top_k, codes.shape, codes.dtype, codes.is_contiguous(), scales.shape, scales.dtype, scales.is_contiguous(),
+           (bias.shape, bias.dtype, bias.is_contiguous()) if bias is not None else None, x.shape, x.stride(), x.dtype, y.shape, y.stride(), y.dtype,
+           plan.shape, plan.dtype, plan.is_contiguous())
     e, n, k, dtype, x_stride, in_order, size, t, act, gate, y_stride = (
         _mx_plans.get(key) or _mx_plan(key, _check_experts, codes, scales, bias, x, plan, int(top_k), y, activation, gated, x_sorted))
     if workspace is None:
@@ -654,7 +651,8 @@ def aiq_mx_linear_experts(codes, scales, bias, x, plan, top_k, y, activation="no
 
 def aiq_combine_experts(z, weights, plan, E, y, residual=None, stream=None):
     """y [T][H] = residual + the weighted sum of each token's rows of z [T * top_k][H]; weights float32 [T][top_k]; residual as y, which it may be."""
-    key = ("combine", E, _matrix(z), _bytes(weights), _bytes(plan), _matrix(y), _matrix(residual))
+    key = (E, z.shape, z.stride(), z.dtype, weights.shape, weights.dtype, weights.is_contiguous(), plan.shape, plan.dtype, plan.is_contiguous(),
+           y.shape, y.stride(), y.dtype, (residual.shape, residual.stride(), residual.dtype) if residual is not None else None)
     dtype, t, top_k, width, z_stride, size, r_stride, y_stride = (
         _mx_plans.get(key) or _mx_plan(key, _check_combine, z, weights, plan, int(E), y, residual))
     d = z.get_device()

@@ -250,6 +250,7 @@ inline size_t plan_whole_smem(const PlanParams& p, int warps) {
 __global__ void __launch_bounds__(kPlanThreads)
 expert_plan_kernel(const __grid_constant__ PlanParams p, const int* ids) {
   extern __shared__ int2 plan_arrays[];
+  chain_release();
   const int b = blockIdx.x;
   plan_share(p, b, ids + (int64_t)b * p.block_tokens * p.top_k, reinterpret_cast<int*>(plan_arrays), [&](int2* at, int* before, int* scratch) {
     const int words = (p.E + 1) / 2, groups = min(16, (int)blockDim.x / words), w = threadIdx.x % words, g = threadIdx.x / words;
@@ -282,10 +283,11 @@ expert_plan_kernel(const __grid_constant__ PlanParams p, const int* ids) {
 
 // Given ids: their counts (first launch of a large plan), or all of a small one.
 __global__ void __launch_bounds__(kPlanThreads)
-expert_count_kernel(const __grid_constant__ PlanParams p, const int* __restrict__ ids) {
+expert_count_kernel(const __grid_constant__ PlanParams p, const int* ids) {
   extern __shared__ int2 plan_arrays[];
   int* smem = reinterpret_cast<int*>(plan_arrays);
   chain_release();
+  chain_wait();
   const int b = blockIdx.x, slot0 = b * p.block_tokens * p.top_k, pairs = min(p.T - b * p.block_tokens, p.block_tokens) * p.top_k;
   if (p.token_blocks == 1) {
     for (int i = threadIdx.x; i < pairs; i += blockDim.x) smem[i] = ids[i];
@@ -750,6 +752,7 @@ __global__ void __launch_bounds__(kPlanThreads)
 route_experts_kernel(const __grid_constant__ RouteParams r, const __grid_constant__ PlanParams p) {
   extern __shared__ __align__(16) float route_smem[];
   chain_release();
+  chain_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5, b = blockIdx.x, token = lane / L;
   // every warp's arrays; biases; the plan's arrays; counts or ids
   const int row = route_row(p.E);
@@ -834,7 +837,7 @@ aiq_status_t launch_route(RouteParams r, const PlanParams& p, cudaStream_t s) {
   }
   {
     LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 10.0 * p.T * p.E, (double)p.T * (p.E * sizeof(T) + 8.0 * p.top_k));
-    route_experts_kernel<T, K, L><<<p.token_blocks, 32 * warps, smem, s>>>(r, p);
+    AIQ_CUDA_TRY(launch_chained(true, route_experts_kernel<T, K, L>, dim3(p.token_blocks), dim3(32 * warps), smem, s, r, p));
     AIQ_LAUNCH_CHECK("route_experts");
   }
   return r.with_plan && !all ? launch_plan(p, r.ids, s) : AIQ_OK;
@@ -865,10 +868,12 @@ constexpr int kCombineThreads = 256;
 // token's order.  A place without an expert counts as a row of zeros.
 template <typename T, int C>
 __global__ void __launch_bounds__(kCombineThreads)
-combine_kernel(const T* __restrict__ z, int64_t z_stride, const float* __restrict__ weights, const int* __restrict__ header, int tokens, int kind,
-               const int* __restrict__ positions, int top_k, int H, const T* residual, int64_t r_stride, T* y, int64_t y_stride) {
+combine_kernel(const T* z, int64_t z_stride, const float* weights, const int* header, int tokens, int kind, const int* positions, int top_k, int H,
+               const T* residual, int64_t r_stride, T* y, int64_t y_stride) {
+  chain_release();
   const int c = (blockIdx.y * kCombineThreads + threadIdx.x) * C;
   if (c >= H) return;
+  chain_wait();
   {
     const int64_t t = blockIdx.x;
     const bool ours = header[2] == tokens && header[3] == kind;
@@ -923,10 +928,10 @@ aiq_status_t launch_combine(const void* z, int64_t z_stride, const float* weight
   if (grid.y > 65535) return set_error(AIQ_ERR_SHAPE, "combine_experts: rows of %d", H);
   LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * tokens * top_k * H, (double)sizeof(T) * tokens * H * (top_k + (residual ? 2 : 1)));
   auto go = [&](auto kernel) {
-    kernel<<<grid, kCombineThreads, 0, s>>>(static_cast<const T*>(z), z_stride, weights, p.header, tokens, plan_kind(top_k, p.E), p.positions, top_k, H,
-                                            static_cast<const T*>(residual), r_stride, static_cast<T*>(y), y_stride);
+    return launch_chained(true, kernel, grid, dim3(kCombineThreads), 0, s, static_cast<const T*>(z), z_stride, weights, p.header, tokens,
+                          plan_kind(top_k, p.E), p.positions, top_k, H, static_cast<const T*>(residual), r_stride, static_cast<T*>(y), y_stride);
   };
-  if (wide) go(combine_kernel<T, 8>); else go(combine_kernel<T, 1>);
+  AIQ_CUDA_TRY(wide ? go(combine_kernel<T, 8>) : go(combine_kernel<T, 1>));
   AIQ_LAUNCH_CHECK("combine_experts");
   return AIQ_OK;
 }
@@ -991,7 +996,7 @@ extern "C" aiq_status_t aiq_plan_experts(const int32_t* ids, int T, int top_k, i
   AIQ_ENSURE_DYNAMIC_SMEM(expert_count_kernel, props.smem_optin);
   const int threads = p.pairs <= kFewPairs ? (p.pairs + 31) / 32 * 32 : kPlanThreads;
   const size_t smem = p.token_blocks > 1 ? sizeof(int) * (size_t)E : sizeof(int) * (((size_t)p.pairs + 3) & ~(size_t)3) + plan_whole_smem(p, threads / 32);
-  expert_count_kernel<<<p.token_blocks, threads, smem, s>>>(p, ids);
+  AIQ_CUDA_TRY(launch_chained(true, expert_count_kernel, dim3(p.token_blocks), dim3(threads), smem, s, p, ids));
   AIQ_LAUNCH_CHECK("expert_count");
   return p.token_blocks > 1 ? launch_plan(p, ids, s) : AIQ_OK;
 }
@@ -1104,5 +1109,6 @@ extern "C" aiq_status_t aiq_mx_linear_experts(const void* codes, const void* sca
   p.tokens = T;
   p.blocks = reinterpret_cast<const aiq::ExpertBlock*>(w + l.blocks);
   p.positions = x_sorted ? nullptr : w + l.positions;
+  p.slots = w + l.slots;
   return aiq::launch_mx_linear_experts(p, workspace, (cudaStream_t)stream);
 }

@@ -43,6 +43,7 @@ struct MxProduct {
   int tokens, plan_kind;      //   what tells that it is one of these sizes
   const ExpertBlock* blocks;
   const int* positions;       // [M / top_k][top_k] rows of each token, or nullptr: x has the plan's rows
+  const int* slots;           // [M] tokens of the rows, times top_k and more
 };
 
 // ---- launchers ------------------------------------------------------------------------
@@ -58,6 +59,7 @@ aiq_status_t launch_mx_product_tc(const MxProduct& p, void* workspace, cudaStrea
 aiq_status_t launch_mx_linear_act_rows(const MxProduct& p, cudaStream_t s);
 aiq_status_t launch_mx_linear_act_tc(const MxProduct& p, void* workspace, cudaStream_t s);        // mx_act.cu
 aiq_status_t launch_mx_linear_experts(const MxProduct& p, void* workspace, cudaStream_t s);       // mx_experts.cu
+aiq_status_t launch_mx_few(const MxProduct& p, cudaStream_t s, bool* done);                       // mx_few.cu: up to four rows, or done = false
 void mx_tc_expire_next(int64_t limit_cycles);      // see aiq_debug_mx_expire_wait
 long long mx_tc_expire_cycles();
 struct MxExpireOnce {                               // held by a call that took the request up

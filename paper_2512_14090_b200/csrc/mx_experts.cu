@@ -5,6 +5,9 @@ namespace aiq {
 
 aiq_status_t launch_mx_linear_experts(const MxProduct& p, void* workspace, cudaStream_t s) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
+  bool done;
+  if (aiq_status_t st = launch_mx_few(p, s, &done)) return st;
+  if (done) return AIQ_OK;
   MxExpireOnce once;
   switch (p.dtype) {
     case AIQ_DTYPE_F32: return launch_kind<1, float, 2>(p, ws, s);

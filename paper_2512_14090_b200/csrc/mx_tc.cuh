@@ -945,9 +945,12 @@ static_assert(kSplitWords % 2 == 0, "a warp takes whole groups of 512 k, as rows
 // the small ones (8192 x 8192, one row 14.0 us either way; 5671 x 609, 37 rows, half 8.7 instead of 8.6).
 template <typename T>
 __global__ void __launch_bounds__(kSplitThreads)
-mx_split_x_kernel(const T* __restrict__ x, int64_t x_stride, int K, int64_t M, int vec, uint32_t segments, FastDiv per_row, int words, int scale_row,
-                  uint2* __restrict__ planes, uint8_t* __restrict__ scales) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+mx_split_x_kernel(const T* x, int64_t x_stride, int K, int64_t M, int vec, uint32_t segments, FastDiv per_row, int words, int scale_row,
+                  uint2* planes, uint8_t* scales) {
+  // In MODE 1 and 2 itself a dependent launch.  The product may begin once every block here is behind the wait: weights and plan, which it reads before
+  // its own wait, are then there whoever wrote them.
+  chain_wait();
+  chain_release();
   const uint32_t seg = blockIdx.x * (kSplitThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (seg >= segments) return;
@@ -979,14 +982,14 @@ int x_vec(const MxProduct& p) {
 }
 
 template <typename T>
-aiq_status_t split_x(const MxProduct& p, uint8_t* planes, uint8_t* scales, cudaStream_t s) {
+aiq_status_t split_x(const MxProduct& p, uint8_t* planes, uint8_t* scales, bool chained, cudaStream_t s) {
   const int words = (int)(mx_plane_row(p.K) / 8);
   const uint32_t per_row = (uint32_t)((words + 32 * kSplitWords - 1) / (32 * kSplitWords));
   const uint64_t segments = (uint64_t)p.M * per_row, blocks = (segments + kSplitThreads / 32 - 1) / (kSplitThreads / 32);
   if (segments > 0x7FFFFF00) return set_error(AIQ_ERR_SHAPE, "mx_split_x: M=%d K=%d", p.M, p.K);     // x and its pieces would be over 1.5 TB
-  mx_split_x_kernel<T><<<(unsigned)blocks, kSplitThreads, 0, s>>>(static_cast<const T*>(p.x), p.x_stride, p.K, p.M, x_vec<T>(p), (uint32_t)segments,
-                                                                   FastDiv(per_row), words, (int)mx_scale_row_bytes(p.K),
-                                                                   reinterpret_cast<uint2*>(planes), scales);
+  AIQ_CUDA_TRY(launch_chained(chained, mx_split_x_kernel<T>, dim3((unsigned)blocks), dim3(kSplitThreads), 0, s, static_cast<const T*>(p.x), p.x_stride, p.K,
+                              (int64_t)p.M, x_vec<T>(p), (uint32_t)segments, FastDiv(per_row), words, (int)mx_scale_row_bytes(p.K),
+                              reinterpret_cast<uint2*>(planes), scales));
   AIQ_LAUNCH_CHECK("mx_split_x");
   return AIQ_OK;
 }
@@ -995,10 +998,12 @@ aiq_status_t split_x(const MxProduct& p, uint8_t* planes, uint8_t* scales, cudaS
 // experts; x in the plan's order already: to the row itself, where the plan has one.
 template <typename T>
 __global__ void __launch_bounds__(kSplitThreads)
-mx_split_pairs_kernel(const T* __restrict__ x, int64_t x_stride, int K, int64_t capacity, int vec, uint32_t segments, FastDiv per_row, int words,
-                      int scale_row, int top_k, const int* __restrict__ header, int tokens, int plan_kind, const int* __restrict__ positions,
-                      uint2* __restrict__ planes, uint8_t* __restrict__ scales) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+mx_split_pairs_kernel(const T* x, int64_t x_stride, int K, int64_t capacity, int vec, uint32_t segments, FastDiv per_row, int words,
+                      int scale_row, int top_k, const int* header, int tokens, int plan_kind, const int* positions, uint2* planes, uint8_t* scales) {
+  // In MODE 1 and 2 itself a dependent launch.  The product may begin once every block here is behind the wait: weights and plan, which it reads before
+  // its own wait, are then there whoever wrote them.
+  chain_wait();
+  chain_release();
   const uint32_t seg = blockIdx.x * (kSplitThreads / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   if (seg >= segments) return;
@@ -1032,9 +1037,9 @@ aiq_status_t split_pairs(const MxProduct& p, uint8_t* planes, uint8_t* scales, c
   const uint32_t per_row = (uint32_t)((words + 32 * kSplitWords - 1) / (32 * kSplitWords));
   const uint64_t segments = (uint64_t)rows * per_row, blocks = (segments + kSplitThreads / 32 - 1) / (kSplitThreads / 32);
   if (segments > 0x7FFFFF00) return set_error(AIQ_ERR_SHAPE, "mx_split_pairs: %d rows, K=%d", rows, p.K);
-  mx_split_pairs_kernel<T><<<(unsigned)blocks, kSplitThreads, 0, s>>>(static_cast<const T*>(p.x), p.x_stride, p.K, p.M, x_vec<T>(p), (uint32_t)segments,
-                                                                       FastDiv(per_row), words, (int)mx_scale_row_bytes(p.K), p.positions ? p.top_k : 1,
-                                                                       p.header, p.tokens, p.plan_kind, p.positions, reinterpret_cast<uint2*>(planes), scales);
+  AIQ_CUDA_TRY(launch_chained(true, mx_split_pairs_kernel<T>, dim3((unsigned)blocks), dim3(kSplitThreads), 0, s, static_cast<const T*>(p.x), p.x_stride, p.K,
+                              (int64_t)p.M, x_vec<T>(p), (uint32_t)segments, FastDiv(per_row), words, (int)mx_scale_row_bytes(p.K), p.positions ? p.top_k : 1,
+                              p.header, p.tokens, p.plan_kind, p.positions, reinterpret_cast<uint2*>(planes), scales));
   AIQ_LAUNCH_CHECK("mx_split_pairs");
   return AIQ_OK;
 }
@@ -1222,7 +1227,7 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   if constexpr (MODE == 2) {
     if (aiq_status_t st = split_pairs<T>(g, workspace, workspace + (size_t)p.pieces * M * mx_plane_row(g.K), s)) return st;
   } else if (KIND == 1) {
-    if (aiq_status_t st = split_x<T>(g, workspace, workspace + (size_t)p.pieces * M * mx_plane_row(g.K), s)) return st;
+    if (aiq_status_t st = split_x<T>(g, workspace, workspace + (size_t)p.pieces * M * mx_plane_row(g.K), MODE == 1, s)) return st;
   }
   // The CTAs of a cluster wait for one another, and each waits for tensor memory, for as long as another CTA on its SM holds it.  If that
   // one belonged to a cluster of another stream with a CTA in the same position elsewhere, neither would ever go on.  So a CTA of a
