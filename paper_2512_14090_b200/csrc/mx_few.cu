@@ -4,8 +4,9 @@
 // to a byte each.  So x is cut into more and smaller pieces, which every CTA makes itself while its first weights are on their way, and both operands are
 // four-bit codes: kind::mxf4, 64 k per MMA, weights as they are stored.
 //   A value is a fixed-point number in units of 2^(e - 3(P - 1)), 2^e <= the largest |x| of its block of 32 < 2^(e + 1), and P digits of it, of -4 to 3, each an
-//   element of the format: with 4 added in every place the digits are three bits each.  P rows of the B operand, with scale bytes e, e - 3, ...  8, 10 and
-//   13 digits hold a bfloat16, half and float exactly, unless it lies below 2^-22, 2^-28, 2^-37 of the block's largest value, or 2^-128.
+//   element of the format: with 4 added in every place the digits are three bits each.  P rows of the B operand, with the scale bytes of a quarter of e's, of
+//   that less 3, ... (a quarter, since the first digit of the largest floats is 2^128); sums are multiplied by 4.  8, 10 and 13 digits hold a bfloat16, half and
+//   float exactly, but for what lies below 2^-22, 2^-28, 2^-37 of the block's largest value, or 2^-126.
 //   D[128 channels][row of x, digit], rows of B to a multiple of 16; the digits' sums are added up smallest first.
 // A CTA takes 128 channels of a layer (or of one expert), and with a cluster a part of K; sums meet in the first CTA of the cluster, in a fixed order.
 //   warp 0      TMA: weights and their scale bytes
@@ -64,7 +65,7 @@ __device__ __forceinline__ void to_digits(const T* row, int k, int K, int vec, i
   for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(f[j]) & 0x7FFFFFFFu);
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   const bool dead = (top >> 23) == 255;            // a NaN or an infinity: scale byte 255 makes the block NaN
-  const int e = max((int)(top >> 23), 3 * (P - 1)), up = 3 * (P - 1) + 127 - e;      // of the value's unit 2^-up
+  const int e = max((int)(top >> 23), 3 * (P - 1) + 2), up = 3 * (P - 1) + 127 - e;      // of the value's unit 2^-up
   // 2^up as two factors, both in range
   const float a = __uint_as_float((uint32_t)((up >> 1) + 127) << 23), b = __uint_as_float((uint32_t)(up - (up >> 1) + 127) << 23);
   constexpr U BIAS = (U)(0x4924924924924924ull & ((1ull << 3 * P) - 1));
@@ -95,7 +96,7 @@ __device__ __forceinline__ void to_digits(const T* row, int k, int K, int vec, i
     }
     const int r = b_row + q;
     *reinterpret_cast<uint2*>(to + r * 128 + ((unit ^ (r & 7)) << 4)) = dead ? make_uint2(0u, 0u) : make_uint2(w[0], w[1]);
-    if (!(lane & 1)) scales[r * 16 + (lane >> 1)] = (uint8_t)(dead ? 255 : e - 3 * q);
+    if (!(lane & 1)) scales[r * 16 + (lane >> 1)] = (uint8_t)(dead ? 255 : e - 2 - 3 * q);
   }
 }
 
@@ -125,16 +126,16 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
 
   // What needs nothing from the kernels before runs beside them (programmatic dependent launch); no global memory is touched before the wait.
-  auto init_barriers = [&]() {
-    // arrivals: four warps for scale bytes read, scale words written and sums read, one for everything else
-    for (int i = lane; i < 2 * p.stages + 2 * kFewScaleStages + 9; i += 32) {
+  if (warp == 0) {
+    // arrivals: four warps for scale bytes read, scale words written and sums read, p.M for a super's digits, one for everything else
+    const int total = 2 * p.stages + 2 * kFewScaleStages + 9;
+    for (int i = lane; i < total + few_supers(p); i += 32) {
       const int j = i - 2 * p.stages;
       const bool four = (j >= kFewScaleStages && j < 2 * kFewScaleStages + 2) || (j >= 2 * kFewScaleStages + 6 && j < 2 * kFewScaleStages + 8);
-      mbar_init(a_full + 8 * i, four ? 4 : 1);
+      mbar_init(a_full + 8 * i, i >= total ? p.M : four ? 4 : 1);
     }
-  };
-  if (warp == 0) {
-    init_barriers();
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncwarp();
     if (lane == 0) {
       s_abort[0] = 0; s_abort[1] = p.limit;
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a_map)) : "memory");
@@ -161,9 +162,11 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   const int n0 = n_block * 128;
 
   // As many rows of x at a time as there are tokens.  (A second time only where tokens have the same expert twice.)
-  for (int m0 = begin; m0 < stop; m0 = p.common ? stop : m0 + p.M) {
-  const int end = p.common ? stop : min(stop, m0 + p.M), x_rows = p.common ? p.M : end - m0;
+  // Rings and phases go on from one time to the next.
   RingCursor ar, sr;
+  uint32_t times = 0, sets = 0, ring = 0, ring_phase = 0;                    // sets: of 512 k so far; ring: of the warp's own
+  for (int m0 = begin; m0 < stop; m0 = p.common ? stop : m0 + p.M, ++times) {
+  const int end = p.common ? stop : min(stop, m0 + p.M), x_rows = p.common ? p.M : end - m0;
   int sent = 0, scales_sent = 0;
   auto send_a = [&]() {
     tma_fill_4d(smem_u32(aring) + ar.stage * kMxATile, &a_map, a_full + 8 * ar.stage, kMxATile, (c_begin + sent) * 128, 0, n0 >> p.gated, expert);
@@ -175,15 +178,7 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
     sr.sent(kFewScaleStages);
     ++scales_sent;
   };
-  if (warp == 0) {
-    if (m0 != begin) {                             // everything once more
-      for (int i = lane; i < 2 * p.stages + 2 * kFewScaleStages + 9 + few_supers(p); i += 32)
-        asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(a_full + 8 * i) : "memory");
-      init_barriers();
-    }
-    for (int i = lane; i < few_supers(p); i += 32) mbar_init(x_full + 8 * i, x_rows);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    __syncwarp();
+  if (warp == 0 && times == 0) {
     if (supers > 0) send_scales();
     while (sent < chunks && sent < p.stages) send_a();
   }
@@ -213,9 +208,9 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
     constexpr uint32_t DESC_HI = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);   // SBO 1024, version 1, 128-byte swizzle
     constexpr uint32_t LBO_FIELD = 1u << 16;
     const uint32_t idesc = (1u << 7) | (1u << 10) | (1u << 23) | (1u << 27) | ((uint32_t)(p.b_rows >> 3) << 17);
-    uint32_t as = 0, aph = 0;
-    for (int s = 0; s < supers && alive; ++s) {
-      const uint32_t tb = s & 1, tph = (s >> 1) & 1;
+    uint32_t as = ring, aph = ring_phase;
+    for (int s = 0; s < supers && alive; ++s, ++sets) {
+      const uint32_t tb = sets & 1, tph = (sets >> 1) & 1;
       if (PROMOTE) alive = mbar_wait_uniform(d_empty + 8 * tb, tph ^ 1u, s_abort);
       alive = alive && mbar_wait_uniform(t_full + 8 * tb, tph, s_abort);       // behind the digits, too
       const uint32_t d = tmem_base + (PROMOTE ? tb * p.b_rows : 0), sf = tmem_base + p.sf_col + tb * 32;
@@ -233,18 +228,19 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       umma_commit(t_empty + 8 * tb);
       if (PROMOTE || s + 1 == supers) umma_commit(d_full + 8 * (PROMOTE ? tb : 0));
     }
+    ring = as; ring_phase = aph;
     if (!alive) {                                  // what was issued must end before the CTA does
       umma_commit(retired);
       const long long t0 = clock64();
       while (!mbar_try_wait(retired, 0) && clock64() - t0 < kWaitLimitCycles) {}
     }
   } else if (warp >= 4) {
-    for (int i = warp - 4; i < supers * x_rows; i += 8) {
-      const int s = i / x_rows, r = i - s * x_rows;
+    for (int i = warp - 4; i < supers * p.M; i += 8) {
+      const int s = i / p.M, r = i - s * p.M;
       int64_t row = r;                             // of x
       if (header && !p.common) row = m0 + r;
       const int half = lane >> 4;                  // a super is two chunks, 16 lanes each
-      to_digits<T>(x + row * p.x_stride, (c_begin / 2 + s) * 512 + lane * 16, p.K, p.vec, lane, digits + (2 * s + half) * p.b_rows * 128, r * P, sb + s * 2048);
+      if (r < x_rows) to_digits<T>(x + row * p.x_stride, (c_begin / 2 + s) * 512 + lane * 16, p.K, p.vec, lane, digits + (2 * s + half) * p.b_rows * 128, r * P, sb + s * 2048);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(x_full + 8 * s);
@@ -252,10 +248,10 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
     if (warp < 8) {
       // ---- scale bytes -> tensor memory: as in mx_tc.cuh, eight columns per 128 k -----------------------
       const uint32_t quarter = (uint32_t)(warp & 3) * 32;
-      uint32_t stage = 0, phase = 0;
-      for (int s = 0; s < supers; ++s) {
-        const uint32_t tb = s & 1, tph = (s >> 1) & 1;
-        alive = mx_wait(s_full + 8 * stage, phase, s_abort) && mx_wait(x_full + 8 * s, 0, s_abort) && mx_wait(t_empty + 8 * tb, tph ^ 1u, s_abort);
+      uint32_t stage = ring, phase = ring_phase;
+      for (int s = 0; s < supers; ++s, ++sets) {
+        const uint32_t tb = sets & 1, tph = (sets >> 1) & 1;
+        alive = mx_wait(s_full + 8 * stage, phase, s_abort) && mx_wait(x_full + 8 * s, times & 1, s_abort) && mx_wait(t_empty + 8 * tb, tph ^ 1u, s_abort);
         if (!alive) break;
         tc_fence_after();
         const uint32_t dst = tmem_base + p.sf_col + tb * 32 + (quarter << 16);
@@ -277,11 +273,12 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
         }
         if (++stage == kFewScaleStages) { stage = 0; phase ^= 1u; }
       }
+      ring = stage; ring_phase = phase;
     } else {
       // ---- sums: lane = channel ---------------------------------------------------------------------------
       const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-      for (int s = PROMOTE ? 0 : supers - 1; s < supers && s >= 0; ++s) {
-        const uint32_t tb = PROMOTE ? s & 1 : 0, tph = PROMOTE ? (s >> 1) & 1 : 0;
+      for (int s = PROMOTE ? 0 : supers - 1; s < supers && s >= 0; ++s, ++sets) {
+        const uint32_t tb = PROMOTE ? sets & 1 : 0, tph = PROMOTE ? (sets >> 1) & 1 : times & 1;
         alive = mx_wait(d_full + 8 * tb, tph, s_abort);
         if (!alive) break;
         tc_fence_after();
@@ -294,7 +291,7 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
           float part = 0.f;
 #pragma unroll
           for (int q = P - 1; q >= 0; --q) part += __uint_as_float(v[q]);      // the smallest digits first
-          sum[r] += part;
+          sum[r] += part * 4.f;
         }
         tc_fence_before();
         __syncwarp();
