@@ -351,10 +351,6 @@ __device__ __forceinline__ float fast_inverse(float v) {
   return r;
 }
 
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
-__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
-__device__ __forceinline__ double smaller(double a, double b) { return fmin(a, b); }
 __device__ __forceinline__ void larger_first(float& a, float& b) {
   const float x = a;
   a = fmaxf(x, b);
@@ -472,40 +468,37 @@ struct Router {
   }
 
   // What a group counts as, of its best two choices (or logits).
-  template <typename S>
-  __device__ __forceinline__ S group_counts(S first, S second) const {
+  __device__ __forceinline__ float group_counts(float first, float second) const {
     if (r.group_best == 1) return first;
-    if (sizeof(S) == 4 && !bias) {                 // of the softmax only the numerators: the rest is common to all
-      first = first == -INFINITY ? first : S(score((float)first, 1.f));
-      second = second == -INFINITY ? second : S(score((float)second, 1.f));
+    if (!bias) {                                   // of the softmax only the numerators: the rest is common to all
+      first = first == -INFINITY ? first : score(first, 1.f);
+      second = second == -INFINITY ? second : score(second, 1.f);
     }
     return second == -INFINITY ? first : first + second;
   }
-  // the groups' scores in the arithmetic of S, of what is in `choice`
-  template <typename S>
-  __device__ __forceinline__ void score_groups(S* scores) {
+  // the groups' scores, of what is in `choice`
+  __device__ __forceinline__ void score_groups() {
     const int lanes = 1 << r.group_shift, per = L >> r.group_shift, part = sub & (lanes - 1);
     const int begin = r.group_size * part >> r.group_shift, n = (r.group_size * (part + 1) >> r.group_shift) - begin;
     for (int g = sub >> r.group_shift; g < (r.groups + per - 1) / per * per; g += per) {
-      S first = -INFINITY, second = -INFINITY;
+      float first = -INFINITY, second = -INFINITY;
       if (g < r.groups) {
         const int base = g * r.group_size + begin;
         int at = n > 0 ? (int)(threadIdx.x & 31) % n : 0;           // from different places on: other banks
         for (int i = 0; i < n; ++i) {
-          S v = choice[base + at];
-          if (sizeof(S) == 8 && v != -INFINITY) v = score64(logit(base + at)) + (bias ? (double)bias[base + at] : 0.0);
+          const float v = choice[base + at];
           if (++at == n) at = 0;
-          second = larger(second, smaller(first, v));
-          first = larger(first, v);
+          second = fmaxf(second, fminf(first, v));
+          first = fmaxf(first, v);
         }
       }
       for (int o = 1; o < lanes; o <<= 1) {
-        const S f = __shfl_xor_sync(0xffffffffu, first, o), t = __shfl_xor_sync(0xffffffffu, second, o);
-        second = larger(larger(second, t), smaller(first, f));
-        first = larger(first, f);
+        const float f = __shfl_xor_sync(0xffffffffu, first, o), t = __shfl_xor_sync(0xffffffffu, second, o);
+        second = fmaxf(fmaxf(second, t), fminf(first, f));
+        first = fmaxf(first, f);
       }
       first = group_counts(first, second);
-      if (g < r.groups && part == 0) scores[g] = first;
+      if (g < r.groups && part == 0) group_score[g] = first;
     }
   }
   // Groups of 8, 16, 32 or 64: beside each other lie the runs of eight of neighbouring lanes.
@@ -538,31 +531,75 @@ struct Router {
       if ((sub & (runs - 1)) == 0 && (c0 + sub) * 8 < E) group_score[(c0 + sub) >> r.run_shift] = group_counts(first[0], second[0]);
     }
   }
-  // the groups that are taken; false where S cannot tell
-  template <typename S>
-  __device__ __forceinline__ bool take_groups(const S* scores, uint32_t* open) {
+  // The groups that are taken, and of them and of the others those that float32 cannot put on either side.
+  __device__ __forceinline__ void take_groups(uint32_t* taken, uint32_t* unclear) {
     __syncwarp();
     uint32_t in = 0;
     float last = INFINITY, next = -INFINITY;
     for (int g = sub; g < r.groups; g += L) {
-      const S mine = scores[g];
+      const float mine = group_score[g];
       int rank = 0;
       for (int o = 0; o < r.groups; ++o) {
-        const S other = scores[o];
+        const float other = group_score[o];
         rank += other > mine || (other == mine && o < g);
       }
       if (rank < r.top_groups) {
         in |= 1u << g;
-        last = fminf(last, (float)mine);
+        last = fminf(last, mine);
       } else {
-        next = fmaxf(next, (float)mine);
+        next = fmaxf(next, mine);
       }
     }
-    *open = join<L>(in, [](uint32_t a, uint32_t b) { return a | b; });
-    if (sizeof(S) == 8 || !(bias || r.group_best == 2)) return true;
+    *taken = join<L>(in, [](uint32_t a, uint32_t b) { return a | b; });
+    *unclear = 0;
+    if (!(bias || r.group_best == 2)) return;
     last = least_of<L>(last);
     next = most_of<L>(next);
-    return next == -INFINITY || last - next > (bias && !r.sigmoid ? 0x1p-17f : 0x1p-19f) + 0x1p-21f * fabsf(next);
+    const float tolerance = (bias && !r.sigmoid ? 0x1p-17f : 0x1p-19f) + 0x1p-21f * fabsf(next);
+    const bool clear = next == -INFINITY || last - next > tolerance;           // (of this token: its lanes stay with the others of the warp)
+    uint32_t near = 0;
+    for (int g = sub; g < r.groups; g += L) {
+      const float mine = group_score[g];
+      if (!clear && mine != -INFINITY && !(in >> g & 1u ? mine - next > tolerance : last - mine > tolerance)) near |= 1u << g;
+    }
+    *unclear = join<L>(near, [](uint32_t a, uint32_t b) { return a | b; });
+  }
+  // Those again in float64, all lanes of a token at one group: the best of them get the places that the others leave.
+  __device__ __forceinline__ uint32_t take_unclear(uint32_t taken, uint32_t unclear) {
+    need64();
+    __syncwarp();
+    for (uint32_t m = unclear; __any_sync(0xffffffffu, m != 0); m &= m - 1) {
+      const int g = __ffs(m) - 1;
+      double first = -INFINITY, second = -INFINITY;
+      if (g >= 0)
+        for (int e = g * r.group_size + sub; e < (g + 1) * r.group_size; e += L)
+          if (choice[e] != -INFINITY) {
+            const double v = score64(logit(e)) + (bias ? (double)bias[e] : 0.0);
+            second = fmax(second, fmin(first, v));
+            first = fmax(first, v);
+          }
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) {
+        const double f = __shfl_xor_sync(0xffffffffu, first, o), t = __shfl_xor_sync(0xffffffffu, second, o);
+        second = fmax(fmax(second, t), fmin(first, f));
+        first = fmax(first, f);
+      }
+      if (g >= 0 && sub == 0) precise[g] = r.group_best == 2 && second != -INFINITY ? first + second : first;
+    }
+    __syncwarp();
+    const int places = r.top_groups - __popc(taken & ~unclear);
+    uint32_t in = taken & ~unclear;
+    for (uint32_t m = unclear; m; m &= m - 1) {
+      const int g = __ffs(m) - 1;
+      int rank = 0;
+      for (uint32_t o = unclear; o; o &= o - 1) {
+        const int other = __ffs(o) - 1;
+        rank += precise[other] > precise[g] || (precise[other] == precise[g] && other < g);
+      }
+      if (rank < places) in |= 1u << g;
+    }
+    __syncwarp();
+    return in;
   }
 
   // rank by F's order; lanes share out the candidates
@@ -621,16 +658,11 @@ struct Router {
     if (r.groups > 1) {
       __syncwarp();
       if (r.run_shift >= 0) score_groups_of_runs();
-      else score_groups(group_score);
-      const bool clear = take_groups(group_score, &open);
-      if (__any_sync(0xffffffffu, !clear && live && !bad)) {
-        need64();
-        __syncwarp();
-        uint32_t exact;
-        score_groups(precise);
-        take_groups(precise, &exact);
-        if (!clear) open = exact;
-      }
+      else score_groups();
+      uint32_t unclear;
+      take_groups(&open, &unclear);
+      if (bad || !live) unclear = 0;
+      if (__any_sync(0xffffffffu, unclear != 0)) open = take_unclear(open, unclear);
     }
     float a[K];
 #pragma unroll
