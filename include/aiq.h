@@ -226,8 +226,11 @@ aiq_status_t aiq_mx_matmul(const void* a_codes, const void* a_scales, int M, con
  *                 n < N / 2: the first half of the rows of W are the gates, the second what they multiply (N even)
  * in float32, rounded once.  activation: AIQ_ACT_NONE, _RELU, _RELU6 (see the model description), SILU v / (1 + exp(-v)), GELU v Phi(v) with the
  * normal distribution's Phi, or GELU_TANH, its approximation v / (1 + exp(-2 sqrt(2/pi) (v + 0.044715 v^3))); a NaN stays one.
- * residual: rows of `dtype`, stride r_stride (ignored for a single row), or NULL; it may be y itself.  The rest as aiq_mx_linear: the
- * three kernels, the same workspace size, workspace NULL. */
+ * residual: rows of `dtype`, stride r_stride (ignored for a single row), or NULL; it may be y itself.  The rest as aiq_mx_linear: its
+ * three kernels, the same workspace size, workspace NULL; but where the third would run and x has up to four (bfloat16), three (half) or two
+ * (float32) rows, a fourth does (it needs no workspace, but has to be given one to be chosen): x as 8, 10 or 13 digits of three bits, which hold it
+ * exactly but for what lies below 2^-22 (bfloat16), 2^-28, 2^-37 of the largest of 32 values, or 2^-126, multiplied on kind::mxf4; sums and waits as in
+ * the third. */
 enum { AIQ_ACT_SILU = 3, AIQ_ACT_GELU = 4, AIQ_ACT_GELU_TANH = 5 };
 aiq_status_t aiq_mx_linear_act(const void* codes, const void* scales, const float* bias, int N, int K, const void* x, int dtype,
                                int M, int64_t x_stride, int activation, int gated, const void* residual, int64_t r_stride,
@@ -272,7 +275,8 @@ aiq_status_t aiq_route_experts(const void* logits, int dtype, int T, int E, int6
 /* y[row] = what aiq_mx_linear_act gives without a residual, with W and bias of the row's expert, for every row of the plan; the other rows of y
  * stay as they are.  codes, scales: [E][N] rows as above, bias float32 [E][N] or NULL, y [T top_k][N, gated: N / 2].
  * x_sorted = 0: x [T][K], a row per token; 1: x [T top_k][K] in the plan's rows (what an earlier call wrote).  x and y may not overlap.
- * On the tensor cores for every size, as the third kernel of aiq_mx_linear (precision, bounded waits); weights of experts without rows are not read.
+ * On the tensor cores for every size, as the third kernel of aiq_mx_linear, or with as few tokens as above the fourth of aiq_mx_linear_act (precision,
+ * bounded waits); weights of experts without rows are not read.
  * workspace: device, 16-byte aligned, aiq_mx_linear_experts_workspace_bytes(E, N, K, T top_k, dtype) bytes, not used by two calls at a time. */
 size_t aiq_mx_linear_experts_workspace_bytes(int E, int N, int K, int rows, int dtype);
 aiq_status_t aiq_mx_linear_experts(const void* codes, const void* scales, const float* bias, int E, int N, int K, const void* x, int dtype,

@@ -350,3 +350,43 @@ def test_a_layer_and_its_graph(dtype, t, top_k, e, d, f):
         got = y.clone()
         _layer(*args)
         assert torch.equal(y, got)
+
+
+def test_a_plan_of_many_token_blocks():
+    """More pairs than the usual number of token blocks may have: against a stable sort."""
+    t, top_k, e = 330_001, 31, 33
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ids = (torch.rand((t, top_k), generator=g, device="cuda") ** 2 * (e + 1)).int() - 1
+    offsets, slots, positions = binding().aiq_expert_plan_parts(plan_of(ids, e), t, top_k, e)
+    flat = ids.reshape(-1).long()
+    order = torch.sort(torch.where(flat < 0, e, flat), stable=True).indices
+    rows = int((flat >= 0).sum())
+    assert int(offsets[-1]) == rows
+    assert torch.equal(offsets.long(), torch.cat((torch.zeros(1, dtype=torch.int64, device="cuda"), torch.bincount(flat[flat >= 0], minlength=e).cumsum(0))))
+    assert torch.equal(slots[:rows].long(), order[:rows]) and (slots[rows:] == -1).all()
+    back = torch.full_like(flat, -1)
+    back[order[:rows]] = torch.arange(rows, device="cuda")
+    assert torch.equal(positions.reshape(-1).long(), back)
+
+
+@pytest.mark.parametrize("t", [3, 40, 300])
+def test_two_streams_at_once(t):
+    """Two layers on two streams, with plans and workspaces of their own, many times over."""
+    b, dt, e, n, k, top_k = binding(), torch.bfloat16, 6, 1024, 2100, 2
+    codes, scales = _experts(e, n, k, 1)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    xs = [activations(t, k, dt, 3 + i) for i in range(2)]
+    ids = [some_ids(t, top_k, e, 5 + i) for i in range(2)]
+    plans = [plan_of(i, e) for i in ids]
+    size = b.aiq_mx_linear_experts_workspace_bytes(e, n, k, t * top_k, dt)
+    ws = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    want = [linear_experts(codes, scales, None, xs[i], plans[i], top_k, torch.empty((t * top_k, n), dtype=dt, device="cuda"), activation="silu") for i in range(2)]
+    ys = [[torch.zeros((t * top_k, n), dtype=dt, device="cuda") for _ in range(10)] for _ in range(2)]
+    torch.cuda.synchronize()
+    for j in range(10):
+        for i in range(2):
+            b.aiq_mx_linear_experts(codes, scales, None, xs[i], plans[i], top_k, ys[i][j], "silu", workspace=ws[i], stream=sides[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for y in ys[i]:
+            assert torch.equal(y, want[i])
