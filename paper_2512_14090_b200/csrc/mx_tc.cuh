@@ -671,6 +671,12 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       const int end = o < outputs ? (MODE == 2 ? at.end : p.M) : 0;
       const int live = min(half, end - m0);                    // this lane's columns that are rows of x
       T* dst = y + (int64_t)m0 * y_stride + n;
+      if constexpr (MODE == 1) {                               // the tile's residual to L2 while its sums are not there yet, a row per thread
+        const int row = at.m0 + (warp - 8) * 32 + lane, o0 = at.n0 >> p.gated;
+        if (direct && ex.residual && row < min(at.m0 + at.Mt, p.M))
+          for (int i = 0; i < min(128 >> p.gated, outputs - o0); i += 128 / (int)sizeof(T))
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(ex.residual + (int64_t)row * ex.r_stride + o0 + i) : "memory");
+      }
       if (PROMOTE) {
         float acc[64];
 #pragma unroll
