@@ -37,6 +37,8 @@
 //
 // MODE: 0 the products as above (mx_tc.cu); 1 one with an activation, a gate and a residual on the way out (mx_act.cu); 2 that for the rows of
 // many experts, each with weights of its own (mx_experts.cu).
+// 3, 4: 1 and 2 for narrow tiles, whose pieces of x are one operand: up to four chunks of 128 k a copy and slot.  (Kernels of their own: with both ways
+// of issuing MMAs in one, gated 8192 x 8192 with 2,048 rows took 235 us instead of 229.)
 // 1, 2: with a gate the weights' copies interleave its two halves, row j of the first beside row j of the second, so that neighbouring lanes
 //   hold what is multiplied: the tensor map has the halves as a dimension of its own, innermost but for k.
 // 2: a tile is 128 channels of one expert and up to Mt of its rows, from the plan's table of blocks of rows (experts.cuh).  The MMA is as wide
@@ -72,7 +74,7 @@ struct MxTcParams {
   int join;                 // MODE 2: a copy brings all pieces of a chunk (up to three fit)
   int ring_rows;            // rows that a slot of the ring for x holds: `rows`, joined those of all pieces
   int n_chunks, supers_per_split;
-  int group;                // MODE 1, 2: chunks per copy and slot of the rings
+  int group;                // MODE 3, 4: chunks per copy and slot of the rings
   int cluster, cluster_log2;
   int push;                 // bytes for sums that the cluster's CTAs write into each other's shared memory; 0: read from it afterwards
   int m_blocks, tiles;      // tiles: row blocks * m_blocks, then the halves of some of them:
@@ -89,7 +91,7 @@ struct MxTcParams {
 };
 
 // what MODE 1 and 2 have beside that
-template <int MODE, typename T>
+template <bool FUSED, typename T>
 struct MxExtra {
   const T* residual;        // [M] rows of `r_stride` elements, or nullptr
   int64_t r_stride;
@@ -97,7 +99,7 @@ struct MxExtra {
   const int* header;
   int tokens, plan_kind;
 };
-template <typename T> struct MxExtra<0, T> {};
+template <typename T> struct MxExtra<false, T> {};
 
 // tile `t` of a launch
 struct MxTile {
@@ -382,8 +384,9 @@ template <int KIND, typename T, bool PROMOTE, int MODE>
 __global__ void __launch_bounds__(kMxTcThreads, 1)
 mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ CUtensorMap sa_map,
              const __grid_constant__ CUtensorMap sb_map, const __grid_constant__ MxTcParams p, const float* __restrict__ bias,
-             T* __restrict__ y, int64_t y_stride, const __grid_constant__ MxExtra<MODE, T> ex) {
+             T* __restrict__ y, int64_t y_stride, const __grid_constant__ MxExtra<(MODE > 0), T> ex) {
   using Kd = MxKind<KIND>;
+  constexpr bool EXPERTS = MODE == 2 || MODE == 4, NARROW = MODE >= 3;
   constexpr bool CHAINED = KIND == 1;              // behind the pre-pass
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -393,26 +396,26 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   const int rank = blockIdx.x & (p.cluster - 1);
   const int first = blockIdx.x >> p.cluster_log2, step = gridDim.x >> p.cluster_log2;      // this CTA's tiles
   const int a_stages = p.a_stages, b_stages = p.b_stages, scale_units = p.stack ? 1 : p.pieces;
-  const int units = MODE == 2 && p.join ? 1 : scale_units;   // copies of a chunk of x
-  const int group = MODE == 0 ? 1 : p.group, a_unit = group * kMxATile;
+  const int units = EXPERTS && p.join ? 1 : scale_units;   // copies of a chunk of x
+  const int group = NARROW ? p.group : 1, a_unit = group * kMxATile;
   const int b_unit = group * mx_b_unit(p.ring_rows), scale_tile = mx_scale_tile(p);
   const int c_begin = min(p.n_chunks, rank * p.supers_per_split * Kd::CPS);
   const int c_end = min(p.n_chunks, c_begin + p.supers_per_split * Kd::CPS);
   const int chunks = c_end - c_begin, supers = (chunks + Kd::CPS - 1) / Kd::CPS;
   const int row_blocks = (p.N + 127) / 128;
   int tiles = p.tiles;
-  if constexpr (MODE == 2) {
+  if constexpr (EXPERTS) {
     const int4 h = *reinterpret_cast<const int4*>(ex.header);
     tiles = h.z == ex.tokens && h.w == ex.plan_kind ? __shfl_sync(0xffffffffu, h.y, 0) * row_blocks : 0;
     if (first >= tiles) return;                    // the whole cluster; nothing has been set up
   }
   auto tile_of = [&](int t) {
-    if constexpr (MODE == 2) return mx_expert_tile(p, ex.blocks, row_blocks, t);
+    if constexpr (EXPERTS) return mx_expert_tile(p, ex.blocks, row_blocks, t);
     else return mx_tile(p, t);
   };
   // copies of rows of x for a tile, and the rows they bring
-  auto boxes_of = [&](const MxTile& at) { return MODE != 2 && at.Mt > p.box ? 2 : 1; };
-  auto rows_of = [&](const MxTile& at) { return MODE == 2 ? p.box : at.Mt; };
+  auto boxes_of = [&](const MxTile& at) { return !EXPERTS && at.Mt > p.box ? 2 : 1; };
+  auto rows_of = [&](const MxTile& at) { return EXPERTS ? p.box : at.Mt; };
 
   uint8_t* aring = smem;
   uint8_t* bring = aring + a_stages * a_unit;
@@ -439,7 +442,9 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   auto send_a = [&]() {
     if constexpr (MODE == 0)
       tma_fill_2d(smem_u32(aring) + ar.stage * kMxATile, &a_map, a_full + 8 * ar.stage, KIND == 0 ? kMxATile : kMxACopied, a_chunk * 128, a_n0);
-    else if (group == 1)
+    else if (MODE == 1)
+      tma_fill_3d(smem_u32(aring) + ar.stage * a_unit, &a_map, a_full + 8 * ar.stage, kMxACopied, a_chunk * 128, 0, a_n0 >> p.gated);
+    else if (!NARROW)
       tma_fill_4d(smem_u32(aring) + ar.stage * a_unit, &a_map, a_full + 8 * ar.stage, kMxACopied, a_chunk * 128, 0, a_n0 >> p.gated, a_expert);
     else
       tma_fill_5d(smem_u32(aring) + ar.stage * a_unit, &a_map, a_full + 8 * ar.stage, group * kMxACopied, 0, 0, a_n0 >> p.gated, a_expert, a_chunk);
@@ -494,16 +499,16 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     RingCursor r;
     for (int tile = first; tile < tiles && alive; tile += step) {
       const MxTile at = tile_of(tile);
-      const int boxes = boxes_of(at), bytes = MODE == 2 || p.stack ? mx_b_unit(p.ring_rows) : rows_of(at) * 128;
+      const int boxes = boxes_of(at), bytes = EXPERTS || p.stack ? mx_b_unit(p.ring_rows) : rows_of(at) * 128;
       for (int c0 = c_begin; c0 < c_end && alive; c0 += Kd::CPS)
         for (int u = units - 1; u >= 0 && alive; --u)
           for (int c = c0; c < min(c0 + Kd::CPS, c_end); c += group) {
             alive = mx_wait(b_empty + 8 * r.stage, r.phase ^ 1u, s_abort);
             if (!alive) break;
             const uint32_t dst = smem_u32(bring) + r.stage * b_unit;
-            if (MODE == 0 || group == 1) tma_fill_3d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)bytes, c * 128, at.m0, u);
+            if (!NARROW) tma_fill_3d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)bytes, c * 128, at.m0, u);
             else tma_fill_4d(dst, &b_map, b_full + 8 * r.stage, (uint32_t)(group * bytes), 0, at.m0, u, c);
-            if (MODE != 2 && boxes == 2) tma_load_3d_elect(dst + p.box * 128, &b_map, b_full + 8 * r.stage, c * 128, at.m0 + p.box, u);
+            if (!EXPERTS && boxes == 2) tma_load_3d_elect(dst + p.box * 128, &b_map, b_full + 8 * r.stage, c * 128, at.m0 + p.box, u);
             r.sent(b_stages);
           }
     }
@@ -547,7 +552,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     bool ready = false, t_ready = false;
     for (int tile = first; tile < tiles && alive; tile += step, ++done) {
       int width = tile < p.full ? p.rows : p.Mt / 2;
-      if constexpr (MODE == 2) width = p.stack ? p.rows : __shfl_sync(0xffffffffu, tile_of(tile).Mt, 0);
+      if constexpr (EXPERTS) width = p.stack ? p.rows : __shfl_sync(0xffffffffu, tile_of(tile).Mt, 0);
       const uint32_t idesc = types | ((uint32_t)(width >> 3) << 17);
       const uint32_t db = p.d_bufs == 2 ? done & 1 : 0, dph = (p.d_bufs == 2 ? done >> 1 : done) & 1;
       if (!PROMOTE && supers > 0) alive = mbar_wait_uniform(d_empty + 8 * db, dph ^ 1u, s_abort);
@@ -580,23 +585,26 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
             const uint32_t na = last ? as : at, naph = last ? aph : atph;
             const bool next_ready = mbar_test(a_full + 8 * na, naph) & mbar_test(b_full + 8 * bs, bph);
             const bool next_t = last && u == 0 ? mbar_test(t_full + 8 * (tb ^ 1u), ((sets + 1) >> 1) & 1) : false;
-            if (MODE == 0 || (MODE == 1 && group == 1)) {
-              mx_mma4<KIND>(d, adesc, bdesc, idesc, sfa, sfb, p.sf_group, accumulate, b_done, a_done);
-            } else {
-              // all of the slot, a joined chunk's pieces one after the other, the smallest first; the last MMAs free the operands
-              const int q0 = MODE == 2 && p.join ? scale_units - 1 : 0, here = min(group, n - cc);
+            if constexpr (NARROW) {
+              // all chunks of the slot; the last MMAs free the operands
+              const int here = min(group, n - cc);
               uint64_t ad = adesc, bd = bdesc;
               uint32_t sa = sfa, sb = sfb;
-              for (int g = 0; g + 1 < here; ++g, ad += kMxATile >> 4, bd += p.ring_rows * 8, sa += p.sf_group, sb += p.sf_group)
-                for (int q = q0; q >= 0; --q) {
-                  mx_mma4_more(d, ad, bd + (uint64_t)(q * p.Mt * 8), idesc, sa, sb + q * p.b_cols, accumulate);
-                  accumulate = 1;
-                }
-              for (int q = q0; q > 0; --q) {
-                mx_mma4_more(d, ad, bd + (uint64_t)(q * p.Mt * 8), idesc, sa, sb + q * p.b_cols, accumulate);
+              for (int g = 0; g + 1 < here; ++g, ad += kMxATile >> 4, bd += p.ring_rows * 8, sa += p.sf_group, sb += p.sf_group) {
+                mx_mma4_more(d, ad, bd, idesc, sa, sb, accumulate);
                 accumulate = 1;
               }
               mx_mma4<KIND>(d, ad, bd, idesc, sa, sb, p.sf_group, accumulate, b_done, a_done);
+            } else {
+              if constexpr (EXPERTS && PieceCount<T>::N <= 3) {
+                // the pieces of a joined chunk, the smallest first
+#pragma unroll
+                for (int q = PieceCount<T>::N - 1; q > 0; --q) {
+                  mx_mma4_more(d, adesc, bdesc + (uint64_t)(q * p.Mt * 8), idesc, sfa, sfb + q * p.b_cols, accumulate);
+                  accumulate = 1;
+                }
+              }
+              mx_mma4<KIND>(d, adesc, bdesc, idesc, sfa, sfb, p.sf_group, accumulate, b_done, a_done);
             }
             accumulate = 1;
             ready = __all_sync(0xffffffffu, next_ready);
@@ -668,10 +676,10 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
       const int outputs = MODE == 0 ? p.N : p.N >> p.gated, o = MODE == 0 ? n : n >> p.gated;
       const int64_t bias_at = MODE == 0 ? n : (int64_t)at.expert * p.N + (p.gated ? (ch & 1) * outputs + o : n);
       const float b = direct && bias && o < outputs ? bias[bias_at] : 0.f;
-      const int end = o < outputs ? (MODE == 2 ? at.end : p.M) : 0;
+      const int end = o < outputs ? (EXPERTS ? at.end : p.M) : 0;
       const int live = min(half, end - m0);                    // this lane's columns that are rows of x
       T* dst = y + (int64_t)m0 * y_stride + n;
-      if constexpr (MODE == 1) {                               // the tile's residual to L2 while its sums are not there yet, a row per thread
+      if constexpr (MODE == 1 || MODE == 3) {                  // the tile's residual to L2 while its sums are not there yet, a row per thread
         const int row = at.m0 + (warp - 8) * 32 + lane, o0 = at.n0 >> p.gated;
         if (direct && ex.residual && row < min(at.m0 + at.Mt, p.M))
           for (int i = 0; i < min(128 >> p.gated, outputs - o0); i += 128 / (int)sizeof(T))
@@ -820,7 +828,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
     if (*s_abort) {                                // a wait that ran out shows in the result
       for (int tile = first; tile < tiles; tile += step) {
         const MxTile at = tile_of(tile);
-        const int shift = MODE == 0 ? 0 : p.gated, end = MODE == 2 ? at.end : p.M, o0 = at.n0 >> shift;
+        const int shift = MODE == 0 ? 0 : p.gated, end = EXPERTS ? at.end : p.M, o0 = at.n0 >> shift;
         const int o_end = min(p.N >> shift, o0 + (128 >> shift));
         for (int i = tid; i < at.Mt * 128; i += kMxTcThreads)
           if (at.m0 + i / 128 < end && o0 + i % 128 < o_end) y[(int64_t)(at.m0 + i / 128) * y_stride + o0 + i % 128] = from_float<T>(__int_as_float(0x7FC00000));
@@ -847,7 +855,7 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
   if (CHAINED) asm volatile("griddepcontrol.wait;" ::: "memory");
   const MxTile at = tile_of(first);
-  const int n0 = at.n0, m0 = at.m0, rows = MODE == 2 ? at.end - m0 : min(p.Mt, p.M - m0);
+  const int n0 = at.n0, m0 = at.m0, rows = EXPERTS ? at.end - m0 : min(p.Mt, p.M - m0);
   const uint32_t copy = ((uint32_t)p.Mt >> p.cluster_log2) * 512;       // push: bytes of one CTA's sums here
   for (int r = rank + warp * p.cluster; r < rows; r += (kMxTcThreads / 32) * p.cluster) {
     T* dst = y + (int64_t)(m0 + r) * y_stride + n0;
@@ -1105,7 +1113,6 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   using Kd = MxKind<KIND>;
   DeviceProps props;
   if (aiq_status_t st = current_device_props(&props)) return st;
-  AIQ_ENSURE_DYNAMIC_SMEM((mx_tc_kernel<KIND, T, PROMOTE, MODE>), props.smem_optin);
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return set_error(AIQ_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
 
@@ -1176,10 +1183,9 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   p.push = p.cluster > 1 && p.Mt <= 64 ? p.Mt * 512 : 0;       // Mt is a multiple of 16, the cluster has 2, 4 or 8 CTAs
   p.supers_per_split = (n_super + p.cluster - 1) / p.cluster;
   if (MODE != 2) p.ring_rows = p.rows;
-  // MODE 1, 2: chunks per copy.  A chunk of a narrow tile is multiplied sooner than its copies and waits are seen to: 16 tokens through 4 of 32 experts
+  // MODE 3, 4: chunks per copy.  A chunk of a narrow tile is multiplied sooner than its copies and waits are seen to: 16 tokens through 4 of 32 experts
   // (4096 x 2048, bfloat16) 35.9 us with one, 32.2 with two, the same with four; 16 rows through 8192 x 8192 17.2, 15.8, 14.7.
-  p.group = 1;
-  if (MODE != 0 && (p.stack || p.join) && p.ring_rows <= 128 && p.supers_per_split * Kd::CPS > 1) p.group = p.ring_rows <= 64 ? 4 : 2;
+  p.group = MODE != 0 && p.stack && p.ring_rows <= 128 ? (p.ring_rows <= 64 ? 4 : 2) : 1;
   const int chunks = (p.supers_per_split * Kd::CPS + p.group - 1) / p.group, units = p.stack || p.join ? 1 : p.pieces;
   p.a_stages = units > 1 ? Kd::CPS / p.group : 2;              // the pieces of one set of chunks read the same weights
   p.b_stages = 2;
@@ -1199,9 +1205,9 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
     const cuuint64_t G = g.gated ? 2 : 1, E = MODE == 2 ? g.experts : 1;
     const cuuint32_t box[5] = {128, (cuuint32_t)G, (cuuint32_t)(128 / G), 1, (cuuint32_t)p.group}, sbox[4] = {16, (cuuint32_t)G, (cuuint32_t)(128 / G), 1};
     // several chunks: the outermost dimension, so that they lie one behind the other in a slot
-    const cuuint64_t dims[5] = {p.group > 1 ? 128 : 2 * w_row, G, N / G, E, (cuuint64_t)p.n_chunks}, strides[4] = {N / G * w_row, w_row, N * w_row, 64};
+    const cuuint64_t dims[5] = {p.stack ? 128 : 2 * w_row, G, N / G, E, (cuuint64_t)p.n_chunks}, strides[4] = {N / G * w_row, w_row, N * w_row, 64};
     const cuuint64_t sdims[4] = {s_row, G, N / G, E}, sstrides[3] = {N / G * s_row, s_row, N * s_row};
-    if (aiq_status_t st = encode(enc, &a_map, KIND == 0 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, g.w_codes, p.group > 1 ? 5 : 4,
+    if (aiq_status_t st = encode(enc, &a_map, KIND == 0 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, g.w_codes, p.stack ? 5 : MODE == 1 ? 3 : 4,
                                  dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
     if (aiq_status_t st = encode(enc, &sa_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.w_scales, 4, sdims, sstrides, sbox, CU_TENSOR_MAP_SWIZZLE_NONE))
       return st;
@@ -1220,7 +1226,7 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
     const uint8_t* codes = KIND == 0 ? g.x_codes : workspace;
 
     const uint8_t* scales = KIND == 0 ? g.x_scales : workspace + P * M * x_row;
-    const bool chunked = p.group > 1;
+    const bool chunked = MODE != 0 && p.stack;
     const cuuint64_t dims[4] = {chunked ? 128 : x_row, M, P, x_row / 128}, strides[3] = {x_row, x_row * M, 128};
     const cuuint32_t box[4] = {128, (cuuint32_t)p.box, (cuuint32_t)(p.stack || p.join ? P : 1), (cuuint32_t)p.group};
     if (aiq_status_t st = encode(enc, &b_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, chunked ? 4 : 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
@@ -1243,7 +1249,7 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   // cluster has its SM to itself: it asks for all of the shared memory.
   const size_t smem = p.cluster > 1 ? (size_t)props.smem_optin : (size_t)mx_smem_bytes(p);
   const int grid = p.cluster > 1 || p.tiles < n_sms ? p.tiles * p.cluster : n_sms;
-  MxExtra<MODE, T> ex = {};
+  MxExtra<(MODE > 0), T> ex = {};
   if constexpr (MODE != 0) {
     ex.residual = static_cast<const T*>(g.residual);
     ex.r_stride = g.r_stride;
@@ -1252,8 +1258,22 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
     ex.tokens = g.tokens;
     ex.plan_kind = g.plan_kind;
   }
-  AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T, PROMOTE, MODE>, dim3(grid), dim3(kMxTcThreads), smem, s, a_map, b_map, sa_map, sb_map, p,
-                                      g.bias, static_cast<T*>(g.y), g.y_stride, ex));
+  auto launch = [&](auto mode) -> aiq_status_t {
+    constexpr int M_ = decltype(mode)::value;
+    AIQ_ENSURE_DYNAMIC_SMEM((mx_tc_kernel<KIND, T, PROMOTE, M_>), props.smem_optin);
+    AIQ_CUDA_TRY(launch_chained_cluster(KIND == 1, p.cluster, mx_tc_kernel<KIND, T, PROMOTE, M_>, dim3(grid), dim3(kMxTcThreads), smem, s, a_map, b_map, sa_map, sb_map,
+                                        p, g.bias, static_cast<T*>(g.y), g.y_stride, ex));
+    return AIQ_OK;
+  };
+  if constexpr (MODE != 0) {
+    if (p.stack) {
+      if (aiq_status_t st = launch(std::integral_constant<int, MODE + 2>())) return st;
+    } else if (aiq_status_t st = launch(std::integral_constant<int, MODE>())) {
+      return st;
+    }
+  } else if (aiq_status_t st = launch(std::integral_constant<int, 0>())) {
+    return st;
+  }
   AIQ_LAUNCH_CHECK("mx_tc");
   return AIQ_OK;
 }
