@@ -440,6 +440,8 @@ __device__ __noinline__ void one_by_one(const T* row, int E, int top_k, bool sig
 // rounding of the exponential's argument and 1 for the exponential (2^-22 of itself), by 3 for 1 + y and the reciprocal; two of them, and the additions of
 // the bias, by 2^-20 + 2^-23 |choice|; two sums of two by 2^-19 and the same.  A softmax has an exponential (4.8), a sum of up to 1024 and a reciprocal:
 // 2^-18, and 2^-17.  Its numerators alone: 2^-19 for two sums of two.
+// Bound by instruction issue and, with one set of tokens for every warp, by the length of the chain: 16,384 tokens among 256 experts, 8 of them, in 8 groups, 22 us
+// (8 MB of logits: 1.3), and 13 for the plan behind it; one token among 32 experts with its plan 4.5 us.
 template <typename T, int K, int L>
 struct Router {
   const RouteParams& r;
@@ -897,7 +899,8 @@ aiq_status_t launch_route(const RouteParams& r, const PlanParams& p, cudaStream_
 constexpr int kCombineThreads = 256;
 
 // A thread has eight neighbouring values of a token (one where rows do not start on 16 bytes).  In float32: residual, then the experts in the
-// token's order.  A place without an expert counts as a row of zeros.
+// token's order.  A place without an expert counts as a row of zeros.  Bound by memory: 4,096 tokens, 8 experts, rows of 4096, bfloat16, residual 61 us (336 MB, 84 %
+// of the copy rate); one token a launch.
 template <typename T, int C>
 __global__ void __launch_bounds__(kCombineThreads)
 combine_kernel(const T* z, int64_t z_stride, const float* weights, const int* header, int tokens, int kind, const int* positions, int top_k, int H,

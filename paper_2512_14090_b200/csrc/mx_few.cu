@@ -15,6 +15,9 @@
 //   warps 4-7   scale bytes: shared -> tensor memory
 //   warps 8-11  sums -> y
 // Two CTAs share an SM, so that one's set-up and way out are covered by the other's stream.
+// What bounds it.  One token through 4 of 32 experts of 4096 x 2048, bfloat16, 7.9 us a call, 8.6 in a graph with weights from memory: a launch, the plan and the first bytes of
+// x and weights one after the other (5 us), then 17.8 MB of weights (2.7 us at the copy rate).  Gated 16384 x 4096, one row 10 us (5.4 for the weights).
+// With the pre-pass and tiles of mx_tc.cuh in its place 12.8 and 14.3.
 #include "mx_tc.cuh"
 
 namespace aiq {
