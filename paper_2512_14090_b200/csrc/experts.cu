@@ -435,11 +435,12 @@ __device__ __noinline__ void one_by_one(const T* row, int E, int top_k, bool sig
 // The choices go to shared memory.  Each lane keeps the K (a power of two, top_k or more) largest, sorted, by merging sorted runs of eight; three
 // exchanges (five) make them the token's.  All experts from the k-th largest on are candidates, which are ranked by comparing each with all.
 // Float32 cannot tell choices apart that are closer than their rounding (equal logits and biases give equal choices): what is that close to
-// the k-th is a candidate, too, and where two are that close, all candidates are ranked in float64; groups likewise, of which the last taken
-// and the first not taken may not be that close.  In steps of 2^-24, scores being at most 1, a logistic function is off by 4.3: by 0.22 for the
+// the k-th is a candidate, too, and where two are that close, all candidates are ranked in float64; groups likewise, of which every taken one has to
+// be clear of every other.  In steps of 2^-24, scores being at most 1, a logistic function is off by 4.3: by 0.22 for the
 // rounding of the exponential's argument and 1 for the exponential (2^-22 of itself), by 3 for 1 + y and the reciprocal; two of them, and the additions of
-// the bias, by 2^-20 + 2^-23 |choice|; two sums of two by 2^-19 and the same.  A softmax has an exponential (4.8), a sum of up to 1024 and a reciprocal:
-// 2^-18, and 2^-17.  Its numerators alone: 2^-19 for two sums of two.
+// the bias, by 2^-20 + 2^-23 |choice|.  A softmax has an exponential (4.8), a sum of up to 1024 and a reciprocal: 2^-18.  A group's sum of two is off by as
+// much, its numerators alone by 2^-20; but what counts of a bias is the size of the two choices, 2^-23 (|first| + |second|) for three roundings, of which the
+// sum may have nothing left where they cancel.
 // Bound by instruction issue and, with one set of tokens for every warp, by the length of the chain: 16,384 tokens among 256 experts, 8 of them, in 8 groups, 22 us
 // (8 MB of logits: 1.3), and 13 for the plan behind it; one token among 32 experts with its plan 4.5 us.
 template <typename T, int K, int L>
@@ -447,7 +448,7 @@ struct Router {
   const RouteParams& r;
   const int E, top_k;
   const float* bias;                               // shared, or nullptr
-  float *choice, *group_score;
+  float *choice, *group_score, *group_size_of;
   Candidate* candidate;
   double* precise;
   int *chosen, *found;
@@ -469,14 +470,19 @@ struct Router {
     sum64 = join<L>(s, [](double a, double b) { return a + b; });
   }
 
-  // What a group counts as, of its best two choices (or logits).
-  __device__ __forceinline__ float group_counts(float first, float second) const {
-    if (r.group_best == 1) return first;
-    if (!bias) {                                   // of the softmax only the numerators: the rest is common to all
-      first = first == -INFINITY ? first : score(first, 1.f);
-      second = second == -INFINITY ? second : score(second, 1.f);
+  // What a group counts as, of its best two choices (or logits), and the size of what was rounded on the way there.
+  __device__ __forceinline__ void put_group(int g, float first, float second) {
+    if (r.group_best == 2) {
+      if (!bias) {                                 // of the softmax only the numerators: the rest is common to all
+        first = first == -INFINITY ? first : score(first, 1.f);
+        second = second == -INFINITY ? second : score(second, 1.f);
+      }
+      if (second == -INFINITY) second = 0.f;
+    } else {
+      second = 0.f;
     }
-    return second == -INFINITY ? first : first + second;
+    group_score[g] = first + second;
+    group_size_of[g] = fabsf(first) + fabsf(second);
   }
   // the groups' scores, of what is in `choice`
   __device__ __forceinline__ void score_groups() {
@@ -499,8 +505,7 @@ struct Router {
         second = fmaxf(fmaxf(second, t), fminf(first, f));
         first = fmaxf(first, f);
       }
-      first = group_counts(first, second);
-      if (g < r.groups && part == 0) group_score[g] = first;
+      if (g < r.groups && part == 0) put_group(g, first, second);
     }
   }
   // Groups of 8, 16, 32 or 64: beside each other lie the runs of eight of neighbouring lanes.
@@ -530,14 +535,17 @@ struct Router {
         second[0] = fmaxf(fmaxf(second[0], t), fminf(first[0], f));
         first[0] = fmaxf(first[0], f);
       }
-      if ((sub & (runs - 1)) == 0 && (c0 + sub) * 8 < E) group_score[(c0 + sub) >> r.run_shift] = group_counts(first[0], second[0]);
+      if ((sub & (runs - 1)) == 0 && (c0 + sub) * 8 < E) put_group((c0 + sub) >> r.run_shift, first[0], second[0]);
     }
   }
   // The groups that are taken, and of them and of the others those that float32 cannot put on either side.
   __device__ __forceinline__ void take_groups(uint32_t* taken, uint32_t* unclear) {
     __syncwarp();
+    // A group's score in float64 is not further than this from what it is here.
+    const float base = bias && !r.sigmoid ? 0x1p-18f : 0x1p-20f;
+    auto off = [&](int g) { return base + 0x1p-22f * group_size_of[g]; };
     uint32_t in = 0;
-    float last = INFINITY, next = -INFINITY;
+    float last = INFINITY, next = -INFINITY;       // the least that a taken one, the most that another can be
     for (int g = sub; g < r.groups; g += L) {
       const float mine = group_score[g];
       int rank = 0;
@@ -547,9 +555,9 @@ struct Router {
       }
       if (rank < r.top_groups) {
         in |= 1u << g;
-        last = fminf(last, mine);
+        last = fminf(last, mine == INFINITY ? mine : mine - off(g));
       } else {
-        next = fmaxf(next, mine);
+        next = fmaxf(next, mine == -INFINITY ? mine : mine + off(g));
       }
     }
     *taken = join<L>(in, [](uint32_t a, uint32_t b) { return a | b; });
@@ -557,12 +565,11 @@ struct Router {
     if (!(bias || r.group_best == 2)) return;
     last = least_of<L>(last);
     next = most_of<L>(next);
-    const float tolerance = (bias && !r.sigmoid ? 0x1p-17f : 0x1p-19f) + 0x1p-21f * fabsf(next);
-    const bool clear = next == -INFINITY || last - next > tolerance;           // (of this token: its lanes stay with the others of the warp)
+    const bool clear = next == -INFINITY || last > next;                       // (of this token: its lanes stay with the others of the warp)
     uint32_t near = 0;
     for (int g = sub; g < r.groups; g += L) {
       const float mine = group_score[g];
-      if (!clear && mine != -INFINITY && !(in >> g & 1u ? mine - next > tolerance : last - mine > tolerance)) near |= 1u << g;
+      if (!clear && mine != -INFINITY && !(in >> g & 1u ? mine - off(g) > next : last > mine + off(g))) near |= 1u << g;
     }
     *unclear = join<L>(near, [](uint32_t a, uint32_t b) { return a | b; });
   }
@@ -815,9 +822,10 @@ route_experts_kernel(const __grid_constant__ RouteParams r, const __grid_constan
   router.sub = lane & (L - 1);
   router.candidate = reinterpret_cast<Candidate*>(at) + token * kCandidates;
   at += (32 / L) * kCandidates * 4;
-  static_assert(kMostGroups <= kCandidates, "groups' scores lie where the candidates' values in 64 bits do");
+  static_assert(kMostGroups <= kCandidates, "two words for each group lie where the candidates' values in 64 bits do");
   router.precise = reinterpret_cast<double*>(at) + token * kCandidates;
   router.group_score = reinterpret_cast<float*>(router.precise);
+  router.group_size_of = router.group_score + kMostGroups;
   at += (32 / L) * kCandidates * 2;
   router.chosen = reinterpret_cast<int*>(at) + token * 32;
   router.found = reinterpret_cast<int*>(at) + (32 / L) * 32 + token;

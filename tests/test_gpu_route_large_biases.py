@@ -1,0 +1,50 @@
+"""Routing with biases far larger than the scores: choices are rounded at the biases' size, so float32 alone cannot order them."""
+import numpy as np
+import pytest
+import torch
+
+from experts_util import new_plan
+from gpu_util import binding
+from oracle import experts_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+def _route(logits, top_k, bias, **how):
+    t, e = logits.shape
+    ids = torch.full((t, top_k), 77, dtype=torch.int32, device="cuda")
+    w = torch.full((t, top_k), 77.0, device="cuda")
+    binding().aiq_route_experts(logits.cuda(), ids, w, bias=bias.cuda(), plan=new_plan(t, top_k, e), **how)
+    return ids.cpu().numpy()
+
+
+def _check(logits, top_k, bias, **how):
+    ids = _route(logits, top_k, bias, **how)
+    want = O.route(logits.double().numpy(), bias.numpy(), top_k=top_k, **how)[0]
+    wrong = (ids != want).any(axis=1)
+    assert not wrong.any(), f"{wrong.sum()} of {len(ids)} tokens, the first {np.flatnonzero(wrong)[0]}"
+
+
+def test_two_best_that_cancel():
+    """In float64 the groups count 1.276519 and 1.277131; with choices rounded to float32 1.277344 and 1.277131."""
+    bias = torch.tensor([3e4, -3e4, -3e4, -3e4, 0, 0, 0, 0])
+    logits = torch.tensor([[0.38631517, -0.17255656, 0.75894272, 0.32788253, 0.68614733, -0.64194930, -1.07925999, 0.45581980]])
+    _check(logits, 2, bias, scoring="sigmoid", groups=2, top_groups=1, group_best=2)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("size", [1.0, 64.0, 1000.0, 2.0 ** 14, 1e5])
+@pytest.mark.parametrize("e,groups,top_groups,top_k", [(16, 8, 3, 4), (64, 8, 3, 8), (48, 4, 2, 6), (12, 6, 5, 3)])
+def test_groups_with_biases_of_both_signs(scoring, size, e, groups, top_groups, top_k):
+    """One expert of every group far up and one as far down (the others at the bottom): the sums of two are as close as scores are."""
+    t, n = 2000, e // groups
+    g = torch.Generator().manual_seed(int(size) + e)
+    bias = torch.full((groups, n), -4 * size)
+    bias[:, 0] = size
+    bias[:, n - 1] = -size
+    logits = 0.5 * torch.randn((t, e), generator=g)
+    for best in (1, 2):
+        _check(logits, top_k, bias.flatten(), scoring=scoring, groups=groups, top_groups=top_groups, group_best=best)
+    # sums of two that float32 cannot tell apart at all
+    logits = 0.5 + torch.randint(-2, 3, (t, e), generator=g) * 2.0 ** -22
+    _check(logits, top_k, bias.flatten(), scoring=scoring, groups=groups, top_groups=top_groups, group_best=2)
