@@ -389,6 +389,9 @@ __host__ __device__ inline int route_warp_words(int E, int L) {
   return 32 / L * (route_row(E) + kCandidates * 4 + kCandidates * 2 + 32) + 4;
 }
 
+// Whether float32 tells two choices with a bias apart: by more than `base` for their scores and the rounding of the additions, at the larger one's size.
+__device__ __forceinline__ bool apart(float x, float y, float base) { return fabsf(x - y) > base + 0x1p-22f * fmaxf(fabsf(x), fabsf(y)); }
+
 // Where a token has more candidates than places (`many`): one after the other from all, by the comparisons that Router makes.  By itself, so that
 // nothing of Router has to lie in memory for it.
 template <typename T, int L>
@@ -405,7 +408,7 @@ __device__ __noinline__ void one_by_one(const T* row, int E, int top_k, bool sig
   };
   auto before = [&](int a, int b) {                // experts that may be chosen
     const float x = choice[a], y = choice[b];
-    if (!bias || fabsf(x - y) > base + 0x1p-22f * fabsf(x)) return x != y ? x > y : a < b;
+    if (!bias || apart(x, y, base)) return x != y ? x > y : a < b;
     if (to_float(row[a]) == to_float(row[b]) && bias[a] == bias[b]) return a < b;
     const double u = exact(a), v = exact(b);
     return u != v ? u > v : a < b;
@@ -740,7 +743,7 @@ struct Router {
     bool near = false;
     rank(n, [&](int j, int i) {
       const Candidate x = candidate[j], y = candidate[i];
-      near = near || (bias && !(fabsf(x.choice - y.choice) > tolerance) && (x.logit != y.logit || x.bias != y.bias));
+      near = near || (bias && !apart(x.choice, y.choice, base) && (x.logit != y.logit || x.bias != y.bias));
       return x.choice > y.choice || (x.choice == y.choice && x.expert < y.expert);
     });
     near = join<L>((int)near, [](int x, int y) { return x | y; });

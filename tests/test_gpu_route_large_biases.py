@@ -48,3 +48,26 @@ def test_groups_with_biases_of_both_signs(scoring, size, e, groups, top_groups, 
     # sums of two that float32 cannot tell apart at all
     logits = 0.5 + torch.randint(-2, 3, (t, e), generator=g) * 2.0 ** -22
     _check(logits, top_k, bias.flatten(), scoring=scoring, groups=groups, top_groups=top_groups, group_best=2)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("size", [16.0, 64.0, 256.0])
+@pytest.mark.parametrize("e,top_k,above", [(24, 3, 2), (64, 6, 2), (64, 8, 6), (200, 31, 20)])
+def test_order_of_choices_with_a_large_bias(scoring, size, e, top_k, above):
+    """Some experts are lifted far above the last one that is chosen, by biases that undo the differences of their scores: their choices are as
+    close as logits can be, and may lie on either side of a float32 number."""
+    t = 3000
+    g = torch.Generator().manual_seed(e)
+    most = 0.8 if scoring == "sigmoid" else 0.8 / above
+    lifted = torch.randperm(e, generator=g)[:above]
+    bias = torch.zeros(e)
+    bias[lifted] = size + 0.5 * most * torch.rand(above, generator=g)
+    p = most * (0.75 + 0.25 * torch.rand((t, 1), generator=g, dtype=torch.float64)) - (bias[lifted].double() - size)
+    if scoring == "sigmoid":
+        logits = torch.full((t, e), -3.0) + torch.randn((t, e), generator=g)
+        logits[:, lifted] = torch.log(p / (1 - p)).float()
+    else:
+        rest = (1 - p.sum(dim=1, keepdim=True)) / (e - above)
+        logits = torch.log(rest).float().repeat(1, e)
+        logits[:, lifted] = torch.log(p).float()
+    _check(logits, top_k, bias, scoring=scoring)
