@@ -1,4 +1,6 @@
 // A layer of experts: which experts a token goes to, the plan that sorts (token, expert) pairs by expert, and the weighted sum of what comes back.
+#include <float.h>
+
 #include "mx.cuh"
 
 namespace aiq {
@@ -484,7 +486,9 @@ struct Router {
     } else {
       second = 0.f;
     }
-    group_score[g] = first + second;
+    // A finite sum beyond float32's range is the range's end, not the infinity that bars a group; its size is infinite then, so that float64 decides.
+    const float most = fabsf(first) < INFINITY ? FLT_MAX : INFINITY;
+    group_score[g] = fminf(fmaxf(first + second, -most), most);
     group_size_of[g] = fabsf(first) + fabsf(second);
   }
   // the groups' scores, of what is in `choice`

@@ -9,6 +9,8 @@ from oracle import experts_oracle as O
 
 pytestmark = pytest.mark.gpu
 
+LOWEST = torch.finfo(torch.float32).min
+
 
 def _route(logits, top_k, bias, **how):
     t, e = logits.shape
@@ -71,3 +73,23 @@ def test_order_of_choices_with_a_large_bias(scoring, size, e, top_k, above):
         logits = torch.log(rest).float().repeat(1, e)
         logits[:, lifted] = torch.log(p).float()
     _check(logits, top_k, bias, scoring=scoring)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("size", [1e9, -LOWEST])
+def test_groups_masked_by_a_large_finite_bias(scoring, size):
+    """Groups of which one or all experts are masked are groups all the same; a sum of two below the lowest float32 is no infinity."""
+    t, e, groups, n = 500, 32, 4, 8
+    g = torch.Generator().manual_seed(3)
+    logits = torch.randn((t, e), generator=g)
+    bias = 0.1 * torch.randn((groups, n), generator=g)
+    bias[3] = -size
+    bias[2, 1:] = -size
+    barred = bias.clone()
+    barred[0] = -np.inf
+    high = bias.clone()
+    high[0, 2:4] = high[1, 5:] = size
+    for b in (bias, barred, high, barred.flip(0), high.flip(0)):
+        for top_groups in (1, 2, 3, 4):
+            for best in (1, 2):
+                _check(logits, 8 * top_groups - 3, b.flatten(), scoring=scoring, groups=groups, top_groups=top_groups, group_best=best)
