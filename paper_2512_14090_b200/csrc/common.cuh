@@ -117,6 +117,15 @@ template <typename... P, typename... A>
 inline cudaError_t launch_chained(bool chain, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A&&... args) {
   return launch_chained_cluster(chain, 1, kernel, grid, block, smem, s, static_cast<A&&>(args)...);
 }
+// Shared memory that a CTA of a cluster asks for, of `bytes` that it uses, where it holds `tmem_cols` of the SM's 512 columns of tensor memory.
+// A CTA waits for its columns as long as others on its SM have them, and the CTAs of a cluster wait for one another while they hold theirs.
+// Two clusters (of two streams) with a CTA each on the same two SMs could so wait for each other without an end, which no limit on a wait breaks.
+// Hence each takes at least the share of the SM's shared memory that its columns are of the tensor memory: whatever mix of such CTAs shares an
+// SM then fits in its tensor memory.  (CTAs without a cluster end by themselves; 1 KB of every CTA's shared memory is the system's.)
+inline size_t cluster_smem(int bytes, int tmem_cols, int smem_optin) {
+  const int64_t sm = (int64_t)smem_optin + 1024, share = (sm * tmem_cols + 511) / 512 - 1024;
+  return (size_t)(share > bytes ? share : bytes);
+}
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // What a kernel of the chain reads of an earlier one's results: an ordinary load, not the read-only path, whose lines
 // may be older than the wait and which the compiler may move above it.  The pointer must not be `const __restrict__` either:

@@ -14,7 +14,7 @@
 //   warps 4-11  x to digits, the warp's next 512 values of a row at a time, 16 a lane; then
 //   warps 4-7   scale bytes: shared -> tensor memory
 //   warps 8-11  sums -> y
-// Two CTAs share an SM, so that one's set-up and way out are covered by the other's stream.
+// Two CTAs (of little K up to four: cluster_smem) share an SM, so that one's set-up and way out are covered by the other's stream.
 // What bounds it.  One token through 4 of 32 experts of 4096 x 2048, bfloat16, 7.9 us a call, 8.6 in a graph with weights from memory: a launch, the plan and the first bytes of
 // x and weights one after the other (5 us), then 17.8 MB of weights (2.7 us at the copy rate).  Gated 16384 x 4096, one row 10 us (5.4 for the weights).
 // With the pre-pass and tiles of mx_tc.cuh in its place 12.8 and 14.3.
@@ -403,7 +403,8 @@ aiq_status_t launch_few(const MxProduct& g, int tiles, FewParams p, const int* s
   if (aiq_status_t st = encode(enc, &a_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.w_codes, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return st;
   if (aiq_status_t st = encode(enc, &sa_map, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.w_scales, 4, sdims, sstrides, sbox, CU_TENSOR_MAP_SWIZZLE_NONE)) return st;
   LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 2.0 * g.M * g.N * g.K, (double)tiles * 128 * (w_row + s_row) + sizeof(T) * (double)g.M * (g.N + g.K));
-  AIQ_CUDA_TRY(launch_chained_cluster(true, p.cluster, mx_few_kernel<T>, dim3(tiles * p.cluster), dim3(kFewThreads), (size_t)few_smem_bytes(p), s, a_map, sa_map, p,
+  const size_t smem = p.cluster > 1 ? cluster_smem(few_smem_bytes(p), p.tmem_cols, props.smem_optin) : (size_t)few_smem_bytes(p);
+  AIQ_CUDA_TRY(launch_chained_cluster(true, p.cluster, mx_few_kernel<T>, dim3(tiles * p.cluster), dim3(kFewThreads), smem, s, a_map, sa_map, p,
                                       static_cast<const T*>(g.x), g.bias, static_cast<const T*>(g.residual), static_cast<T*>(g.y), g.header, g.blocks, slots));
   AIQ_LAUNCH_CHECK("mx_few");
   return AIQ_OK;

@@ -1247,10 +1247,8 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
   } else if (KIND == 1) {
     if (aiq_status_t st = split_x<T>(g, workspace, workspace + (size_t)p.pieces * M * mx_plane_row(g.K), MODE == 1, s)) return st;
   }
-  // The CTAs of a cluster wait for one another, and each waits for tensor memory, for as long as another CTA on its SM holds it.  If that
-  // one belonged to a cluster of another stream with a CTA in the same position elsewhere, neither would ever go on.  So a CTA of a
-  // cluster has its SM to itself: it asks for all of the shared memory.
-  const size_t smem = p.cluster > 1 ? (size_t)props.smem_optin : (size_t)mx_smem_bytes(p);
+  // A CTA of a cluster has its SM to itself: it asks for all of the shared memory, as much as any tensor memory asks for (cluster_smem).
+  const size_t smem = p.cluster > 1 ? cluster_smem(mx_smem_bytes(p), 512, props.smem_optin) : (size_t)mx_smem_bytes(p);
   const int grid = p.cluster > 1 || p.tiles < n_sms ? p.tiles * p.cluster : n_sms;
   MxExtra<(MODE > 0), T> ex = {};
   if constexpr (MODE != 0) {

@@ -576,7 +576,8 @@ aiq_status_t launch_qlinear_tc_bits(const LayerJob& job, int N, int K, int M, vo
                                                                           : qlinear_split_x_kernel<BITS != 32, BITS == 4, false>;
   split_x<<<M, 512, 0, s>>>(x, K, M, planes, down, y, p.atomic ? (long long)M * N : 0ll, status);
   AIQ_LAUNCH_CHECK("qlinear_split_x");
-  const int smem = qt_smem_bytes(T::A_STAGES, p.Mt, p.stack, b_stages, w_stages) + 1024;
+  const int used = qt_smem_bytes(T::A_STAGES, p.Mt, p.stack, b_stages, w_stages) + 1024;
+  const size_t smem = p.cluster > 1 ? cluster_smem(used, p.tmem_cols, smem_limit) : (size_t)used;
   AIQ_CUDA_TRY(launch_chained_cluster(true, p.cluster, qlinear_tc_kernel<BITS>, dim3(row_blocks * p.cluster, groups, m_blocks), dim3(T::THREADS), smem, s,
                               x_map, w_map, p, job.scale, job.bias, (const float*)down, y));
   AIQ_LAUNCH_CHECK("qlinear_tc");
