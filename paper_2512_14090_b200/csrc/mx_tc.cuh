@@ -410,7 +410,11 @@ mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ 
   if constexpr (EXPERTS) {
     const int4 h = *reinterpret_cast<const int4*>(ex.header);
     tiles = h.z == ex.tokens && h.w == ex.plan_kind ? __shfl_sync(0xffffffffu, h.y, 0) * row_blocks : 0;
-    if (first >= tiles) return;                    // the whole cluster; nothing has been set up
+    if (first >= tiles) {                          // the whole cluster; nothing has been set up
+      // Where no CTA has a tile the launch must still not end before the pre-pass, which reads x and the plan: the next kernel waits for this one alone.
+      chain_wait();
+      return;
+    }
   }
   auto tile_of = [&](int t) {
     if constexpr (EXPERTS) return mx_expert_tile(p, ex.blocks, row_blocks, t);
