@@ -192,7 +192,8 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
   // Before a CTA writes into another's shared memory, that one has to have started: arrived here, waited for at the first write.
   if (p.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   const uint32_t tmem_base = __shfl_sync(0xffffffffu, *s_tmem, 0);
-  bool alive = true;
+  bool alive = times == 0 || __shfl_sync(0xffffffffu, s_abort[0], 0) == 0;   // a wait that ran out the time before: nothing is waited for any more
+  const bool began = alive;
   float sum[kFewRows] = {0.f, 0.f, 0.f, 0.f};      // warps 8-11: of this lane's channel
 
   if (warp == 0) {
@@ -232,7 +233,7 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       if (PROMOTE || s + 1 == supers) umma_commit(d_full + 8 * (PROMOTE ? tb : 0));
     }
     ring = as; ring_phase = aph;
-    if (!alive) {                                  // what was issued must end before the CTA does
+    if (began && !alive) {                         // what was issued must end before the CTA does
       umma_commit(retired);
       const long long t0 = clock64();
       while (!mbar_try_wait(retired, 0) && clock64() - t0 < kWaitLimitCycles) {}
@@ -252,7 +253,7 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
       // ---- scale bytes -> tensor memory: as in mx_tc.cuh, eight columns per 128 k -----------------------
       const uint32_t quarter = (uint32_t)(warp & 3) * 32;
       uint32_t stage = ring, phase = ring_phase;
-      for (int s = 0; s < supers; ++s, ++sets) {
+      for (int s = 0; s < supers && alive; ++s, ++sets) {
         const uint32_t tb = sets & 1, tph = (sets >> 1) & 1;
         alive = mx_wait(s_full + 8 * stage, phase, s_abort) && mx_wait(x_full + 8 * s, times & 1, s_abort) && mx_wait(t_empty + 8 * tb, tph ^ 1u, s_abort);
         if (!alive) break;
@@ -280,7 +281,7 @@ mx_few_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__
     } else {
       // ---- sums: lane = channel ---------------------------------------------------------------------------
       const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-      for (int s = PROMOTE ? 0 : supers - 1; s < supers && s >= 0; ++s, ++sets) {
+      for (int s = PROMOTE ? 0 : supers - 1; s < supers && s >= 0 && alive; ++s, ++sets) {
         const uint32_t tb = PROMOTE ? sets & 1 : 0, tph = PROMOTE ? (sets >> 1) & 1 : times & 1;
         alive = mx_wait(d_full + 8 * tb, tph, s_abort);
         if (!alive) break;
