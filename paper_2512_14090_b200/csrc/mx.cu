@@ -320,7 +320,7 @@ struct RowsHeld {
   }
 };
 
-// FUSED: an activation, a gate and a residual on the way out.  With a gate, channel n of a warp is row n / 2 of the weights' first half (n even) or
+// FUSED: an activation, a gate and a residual on the way out.  The residual may be y itself, so y is not __restrict__.  With a gate, channel n of a warp is row n / 2 of the weights' first half (n even) or
 // second half (n odd), so that a gate and its factor are in the same warp.
 struct MxTail {
   int act, gated;
@@ -333,7 +333,7 @@ __device__ __forceinline__ int weight_row(const MxTail& tail, int n, int N) { re
 template <typename X, typename T, int MT, int U, bool FUSED>
 __global__ void __launch_bounds__(kMxThreads)
 mx_product_rows_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t row_bytes, int64_t scale_row,
-                       const float* __restrict__ bias, int N, int K, int M, int k_warps, T* __restrict__ y, int64_t y_stride, MxTail tail) {
+                       const float* __restrict__ bias, int N, int K, int M, int k_warps, T* y, int64_t y_stride, MxTail tail) {
   constexpr int R = kRowChannels, WARPS = kMxThreads / 32;
   __shared__ float part[WARPS][R * MT];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kw = warp % k_warps;
@@ -655,7 +655,7 @@ struct OneHeld {                                 // x microscaled
 template <typename X, typename T, bool FUSED>
 __global__ void __launch_bounds__(32 * kOneWarps, X::P == 1 ? 2 : 1)
 mx_product_row_kernel(X x, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t row_bytes, int64_t scale_row,
-                      const float* __restrict__ bias, int N, int K, int channels, T* __restrict__ y, MxTail tail) {
+                      const float* __restrict__ bias, int N, int K, int channels, T* y, MxTail tail) {
   constexpr int R = kOneRow, P = X::P;
   __shared__ float part[kOneChannels * kOneWarps];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, warps = blockDim.x >> 5;

@@ -96,7 +96,7 @@ struct MxTcParams {
 // what MODE 1 and 2 have beside that
 template <bool FUSED, typename T>
 struct MxExtra {
-  const T* residual;        // [M] rows of `r_stride` elements, or nullptr
+  const T* residual;        // [M] rows of `r_stride` elements, or nullptr; may be y itself, which is therefore not __restrict__
   int64_t r_stride;
   const ExpertBlock* blocks;       // MODE 2: the plan's
   const int* header;
@@ -387,7 +387,7 @@ template <int KIND, typename T, bool PROMOTE, int MODE>
 __global__ void __launch_bounds__(kMxTcThreads, 1)
 mx_tc_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const __grid_constant__ CUtensorMap sa_map,
              const __grid_constant__ CUtensorMap sb_map, const __grid_constant__ MxTcParams p, const float* __restrict__ bias,
-             T* __restrict__ y, int64_t y_stride, const __grid_constant__ MxExtra<(MODE > 0), T> ex) {
+             T* y, int64_t y_stride, const __grid_constant__ MxExtra<(MODE > 0), T> ex) {
   using Kd = MxKind<KIND>;
   constexpr bool EXPERTS = MODE == 2 || MODE == 4, NARROW = MODE >= 3;
   constexpr bool CHAINED = KIND == 1;              // behind the pre-pass
