@@ -341,15 +341,10 @@ template <int L> __device__ __forceinline__ float sum_of(float v) { return join<
 template <int L> __device__ __forceinline__ float most_of(float v) { return join<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
 template <int L> __device__ __forceinline__ float least_of(float v) { return join<L>(v, [](float a, float b) { return fminf(a, b); }); }
 
-// 2^x and 1 / x as the hardware has them
+// exp(x) by 2^x as the hardware has it
 __device__ __forceinline__ float fast_exp(float v) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v * 1.4426950408889634f));
-  return r;
-}
-__device__ __forceinline__ float fast_inverse(float v) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
 

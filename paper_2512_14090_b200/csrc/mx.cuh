@@ -112,6 +112,13 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// 1 / x as the hardware has it
+__device__ __forceinline__ float fast_inverse(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+
 // C values through an AIQ_ACT_*.  Comparisons, not fmaxf: a NaN stays one.  x times a logistic function of x (SILU) or of 2 sqrt(2/pi) (x + 0.044715 x^3),
 // since (1 + tanh u) / 2 = 1 / (1 + exp(-2u)); the error function's complement, so that nothing is cancelled left of zero.  All in float32.
 template <int C>
@@ -125,10 +132,13 @@ __device__ __forceinline__ void mx_activate(float* v, int act) {
 #pragma unroll
     for (int j = 0; j < C; ++j) v[j] = 0.5f * v[j] * erfcf(v[j] * -0.70710678118654752f);
   } else {
+    // exp(u) / (1 + exp(u)): 1 / (1 + exp(-u)) would vanish left of -87, where the reciprocal's argument nears the end of float32's range, and the
+    // result does not until -104.  Right of 80 it is 1.
 #pragma unroll
     for (int j = 0; j < C; ++j) {
       const float u = act == AIQ_ACT_SILU ? v[j] : v[j] * (1.5957691216057308f + 0.071354816272600248f * v[j] * v[j]);
-      v[j] = __fdividef(v[j], 1.f + expf(-u));
+      const float e = expf(fminf(u, 80.f));
+      v[j] *= e * fast_inverse(1.f + e);
     }
   }
 }
