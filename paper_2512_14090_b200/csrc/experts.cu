@@ -36,7 +36,7 @@ PlanLayout plan_layout(int T, int top_k, int E) {
   // Rows per block: twice an expert's share, as long as it gets that many tokens.
   const int share = (l.pairs + E - 1) / E;
   l.width = 16;
-  while (l.width < 128 && l.width < 2 * share && l.width < T) l.width *= 2;
+  while (l.width < 128 && l.width / 2 < share && l.width < T) l.width *= 2;      // (twice the share may be 2^31)
   l.blocks_most = l.pairs / l.width + (l.pairs < E ? l.pairs : E);
   const int even = (T + kTokenBlocks - 1) / kTokenBlocks;
   l.block_tokens = T <= kOneBlockTokens ? T : even < 16 ? 16 : even;
