@@ -846,11 +846,15 @@ route_experts_kernel(const __grid_constant__ RouteParams r, const __grid_constan
   }
 }
 
+// bytes: ids in; slots, positions and offsets out
+double plan_work(const PlanParams& p) { return 4.0 * (3.0 * p.pairs + p.E + 1); }
+
 aiq_status_t launch_plan(const PlanParams& p, const int* ids, cudaStream_t s) {
   const size_t smem = plan_smem(p.E, kPlanThreads / 32);
   DeviceProps props;
   if (aiq_status_t st = current_device_props(&props)) return st;
   AIQ_ENSURE_DYNAMIC_SMEM(expert_plan_kernel, props.smem_optin);
+  LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 0.0, plan_work(p));
   AIQ_CUDA_TRY(launch_chained(true, expert_plan_kernel, dim3(p.token_blocks), dim3(kPlanThreads), smem, s, p, ids));
   AIQ_LAUNCH_CHECK("expert_plan");
   return AIQ_OK;
@@ -1041,8 +1045,11 @@ extern "C" aiq_status_t aiq_plan_experts(const int32_t* ids, int T, int top_k, i
   AIQ_ENSURE_DYNAMIC_SMEM(expert_count_kernel, props.smem_optin);
   const int threads = p.pairs <= kFewPairs ? (p.pairs + 31) / 32 * 32 : kPlanThreads;
   const size_t smem = p.token_blocks > 1 ? sizeof(int) * (size_t)E : sizeof(int) * (((size_t)p.pairs + 3) & ~(size_t)3) + plan_whole_smem(p, threads / 32);
-  AIQ_CUDA_TRY(launch_chained(true, expert_count_kernel, dim3(p.token_blocks), dim3(threads), smem, s, p, ids));
-  AIQ_LAUNCH_CHECK("expert_count");
+  {
+    LaunchScope scope(AIQ_KERNEL_QLINEAR, s, 0.0, p.token_blocks > 1 ? 4.0 * p.pairs : plan_work(p));
+    AIQ_CUDA_TRY(launch_chained(true, expert_count_kernel, dim3(p.token_blocks), dim3(threads), smem, s, p, ids));
+    AIQ_LAUNCH_CHECK("expert_count");
+  }
   return p.token_blocks > 1 ? launch_plan(p, ids, s) : AIQ_OK;
 }
 
