@@ -26,9 +26,11 @@ struct PlanLayout {
 };
 constexpr int kMostPairs = 65535;                // of a token block
 __host__ __device__ inline int plan_kind(int top_k, int E) { return 0x41000000 | top_k << 16 | E; }
-constexpr int kOneBlockTokens = 16;              // up to here one thread block does everything: 32 tokens among 256 experts 15.0 us, in two launches 12.5
+// Up to here one thread block does everything.  Choices and plan, in one launch and in two, calls in a graph: 16 tokens among 256 experts 7.9 us and 9.2, among
+// 32 experts 6.2 and 8.2; 32 tokens 10.4 and 10.2, 5.6 and 8.1; 64 tokens among 256 experts 15.5 and 10.4.
+constexpr int kOneBlockTokens = 16;
 constexpr int kPlanThreads = 1024;
-constexpr int kTokenBlocks = 148;                // with up to kMostPairs each
+constexpr int kTokenBlocks = 148;                // as many as a B200 has SMs: a plan's size is asked for without a device; with up to kMostPairs each
 
 PlanLayout plan_layout(int T, int top_k, int E) {
   PlanLayout l = {};
@@ -378,7 +380,7 @@ struct __align__(16) Candidate {
   float choice, logit, bias;
   int expert;
 };
-constexpr int kFewTokens = 4736;
+constexpr int kFewTokens = kTokenBlocks * kPlanThreads / 32;       // a warp for each token at once
 constexpr int kCandidates = 32;                  // of a token
 // words of shared memory of a warp: choices, candidates, their values in 64 bits or before that the groups' scores, the chosen, counts
 __host__ __device__ inline int route_row(int E) { return (E + 7) / 8 * 8; }
@@ -441,8 +443,9 @@ __device__ __noinline__ void one_by_one(const T* row, int E, int top_k, bool sig
 // the bias, by 2^-20 + 2^-23 |choice|.  A softmax has an exponential (4.8), a sum of up to 1024 and a reciprocal: 2^-18.  A group's sum of two is off by as
 // much, its numerators alone by 2^-20; but what counts of a bias is the size of the two choices, 2^-23 (|first| + |second|) for three roundings, of which the
 // sum may have nothing left where they cancel.
-// Bound by instruction issue and, with one set of tokens for every warp, by the length of the chain: 16,384 tokens among 256 experts, 8 of them, in 8 groups, 22 us
-// (8 MB of logits: 1.3), and 13 for the plan behind it; one token among 32 experts with its plan 4.5 us.
+// Bound by the length of the chain: every warp has one set of tokens, whose choices pass through shared memory five times, and issue is active for 34 % of the
+// time.  16,384 tokens among 256 experts, 8 of them, in 8 groups, 22 us (8 MB of logits: 1.3), and 13 for the plan behind it; one token among 32 experts with its
+// plan 4.5 us.  (64 registers, for blocks of 1,024 threads: 28 to 100 bytes a thread are spilt.)
 template <typename T, int K, int L>
 struct Router {
   const RouteParams& r;

@@ -398,6 +398,7 @@ aiq_status_t launch_few(const MxProduct& g, int tiles, FewParams p, const int* s
   p.hold = expire != 0;
   CUtensorMap a_map, sa_map;
   const cuuint64_t w_row = (cuuint64_t)mx_row_bytes(g.K), s_row = (cuuint64_t)mx_scale_row_bytes(g.K), N = g.N, G = g.gated ? 2 : 1, E = g.experts ? g.experts : 1;
+  // (the order of the strides: see launch_kind in mx_tc.cuh)
   const cuuint32_t box[4] = {128, (cuuint32_t)G, (cuuint32_t)(128 / G), 1}, sbox[4] = {16, (cuuint32_t)G, (cuuint32_t)(128 / G), 1};
   const cuuint64_t dims[4] = {w_row, G, N / G, E}, strides[3] = {N / G * w_row, w_row, N * w_row};
   const cuuint64_t sdims[4] = {s_row, G, N / G, E}, sstrides[3] = {N / G * s_row, s_row, N * s_row};

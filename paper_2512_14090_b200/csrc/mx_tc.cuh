@@ -1212,6 +1212,9 @@ aiq_status_t launch_kind(const MxProduct& g, uint8_t* workspace, cudaStream_t s)
     const cuuint64_t G = g.gated ? 2 : 1, E = MODE == 2 ? g.experts : 1;
     const cuuint32_t box[5] = {128, (cuuint32_t)G, (cuuint32_t)(128 / G), 1, (cuuint32_t)p.group}, sbox[4] = {16, (cuuint32_t)G, (cuuint32_t)(128 / G), 1};
     // several chunks: the outermost dimension, so that they lie one behind the other in a slot
+    // Strides are not in order here: the halves' is larger than the next, the chunks' (64 bytes) the smallest.  A copy adds up coordinate times stride whatever
+    // the order, and the driver takes such maps (encode() reports one that it refuses); the encoder's public description, though, has every stride a multiple of
+    // the one before.  Without this an interleaved copy would be one for every row.
     const cuuint64_t dims[5] = {p.stack ? 128 : 2 * w_row, G, N / G, E, (cuuint64_t)p.n_chunks}, strides[4] = {N / G * w_row, w_row, N * w_row, 64};
     const cuuint64_t sdims[4] = {s_row, G, N / G, E}, sstrides[3] = {N / G * s_row, s_row, N * s_row};
     if (aiq_status_t st = encode(enc, &a_map, KIND == 0 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, g.w_codes, p.stack ? 5 : MODE == 1 ? 3 : 4,
