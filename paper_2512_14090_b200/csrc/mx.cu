@@ -320,8 +320,8 @@ struct RowsHeld {
   }
 };
 
-// FUSED: an activation, a gate and a residual on the way out.  The residual may be y itself, so y is not __restrict__.  With a gate, channel n of a warp is row n / 2 of the weights' first half (n even) or
-// second half (n odd), so that a gate and its factor are in the same warp.
+// FUSED: an activation, a gate and a residual on the way out.  The residual may be y itself, so y is not __restrict__.  With a gate, channel n of a
+// warp is row n / 2 of the weights' first half (n even) or second half (n odd), so that a gate and its factor are in the same warp.
 struct MxTail {
   int act, gated;
   const void* residual;
